@@ -281,6 +281,35 @@ rc_status rc_full_attention_ws(const rc_layout* L, int32_t B, int32_t H, int32_t
  * tiles).  0 on invalid input. */
 size_t rc_full_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D);
 
+/* Gradient of rc_full_attention for training under any mask.  With p_ij =
+ * exp(scale q_i.k_j - lse_i) over the visible pairs, d_o and dlse the
+ * gradients of the outputs, and D_i = d_o_i.o_i - dlse_i:
+ *   ds_ij = p_ij (d_o_i.v_j - D_i)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij d_o_i
+ * The probabilities are recomputed from q, k and the forward's lse; products
+ * take bf16 operands (p and ds rounded once, RNE) and accumulate in fp32.
+ *   q, k, v        as rc_full_attention, token stride tok_stride
+ *   o, d_o         [B, N, H, D] contiguous bf16: the forward's output and the gradient of it
+ *   lse            [B, H, N] fp32: the forward's log-sum-exp
+ *   dlse           [B, H, N] fp32: the gradient of lse, NULL for none
+ *   dq, dk, dv     [B, N, H, D] bf16 out, token stride grad_stride (as tok_stride: views of
+ *                  one fused buffer work); they overlap no input and not each other
+ *   workspace      device, 16-byte aligned, rc_full_backward_workspace_bytes bytes; its
+ *                  contents before and after the call do not matter
+ * Rows that read nothing (lse = -inf) get dq = 0 and add to no key, whatever
+ * their o, d_o and dlse hold; keys that nobody reads get dk = dv = 0.
+ * Deterministic: the sums keep one order.  RC_ERR_WORKSPACE for a missing or small workspace;
+ * RC_ERR_UNSUPPORTED where the mask needs too many merged ranges from either side. */
+rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, int32_t D, float scale,
+                                     const void* q, const void* k, const void* v, int64_t tok_stride,
+                                     const void* o, const float* lse, const void* d_o, const float* dlse,
+                                     void* dq, void* dk, void* dv, int64_t grad_stride,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace rc_full_attention_backward needs: two floats per (batch,
+ * head, row).  0 on invalid input. */
+size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D);
+
 /* FP8 reference cache (the paper calls caching complementary to other
  * accelerations, Sec. 1 and Sec. 4.2; storing the cache in e4m3 halves its bytes,
  * its residency and the step's cached-key traffic).

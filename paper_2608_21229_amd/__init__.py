@@ -11,6 +11,7 @@ residual) through it.
 """
 from .binding import (  # noqa: F401
     Layout, RcError, lib, ref_kv_prefill, step_masked_attention, step_masked_attention_noalloc, full_attention,
+    full_attention_backward,
     linear, NOALLOC_SCRATCH_BYTES,
     ref_kv_prefill_fp8, step_masked_attention_fp8, fp8_cache_shapes,
     SEG_ANCHOR, SEG_TEXT, SEG_TARGET, SEG_REF,

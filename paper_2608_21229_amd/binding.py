@@ -81,6 +81,9 @@ SIGNATURES = {
     "rc_full_workspace_bytes": (_sz, [_PL, _i32, _i32, _i32]),
     "rc_prefill_launch_plan": (_i32, [_PL, _i32, _i32, _i32, ctypes.POINTER(_i64), ctypes.POINTER(_i32),
                                       ctypes.POINTER(_i64)]),
+    "rc_full_backward_workspace_bytes": (_sz, [_PL, _i32, _i32, _i32]),
+    "rc_full_attention_backward": (_i32, [_PL, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
+                                          _vp, _vp, _i64, _vp, _sz, _vp]),
     "rc_status_string": (ctypes.c_char_p, [_i32]),
     "rc_last_error": (ctypes.c_char_p, []),
 }
@@ -174,6 +177,10 @@ class Layout:
     def full_workspace_bytes(self, B: int, H: int, D: int) -> int:
         """Workspace of the full recompute's last-round split (0: no split)."""
         return int(lib().rc_full_workspace_bytes(ctypes.byref(self.c), B, H, D))
+
+    def backward_workspace_bytes(self, B: int, H: int, D: int) -> int:
+        """Workspace of the full recompute's gradient."""
+        return int(lib().rc_full_backward_workspace_bytes(ctypes.byref(self.c), B, H, D))
 
     def prefill_plan(self, B: int, H: int, D: int):
         """(attention work-groups, copy work-groups, cache rows they copy) of
@@ -408,6 +415,39 @@ def full_attention(layout: Layout, q, k, v, o=None, lse=None, scale: Optional[fl
     _call(lib().rc_full_attention_ws, dev, stream, ctypes.byref(layout.c), B, H, D, scale, q.data_ptr(), k.data_ptr(),
           v.data_ptr(), ts, o.data_ptr(), _ptr(lse), _ptr(ws), need)
     return o, lse
+
+
+def full_attention_backward(layout: Layout, q, k, v, o, lse, do, dq=None, dk=None, dv=None, dlse=None,
+                            scale: Optional[float] = None, workspace=None, stream=None):
+    """Gradient of full_attention.  q/k/v, o and lse: the forward's inputs and
+    outputs (want_lse=True); do, dlse (None: zero): the gradients of o and
+    lse.  dq, dk and dv share one token stride (views of one [B, N, 3, H, D]
+    buffer work) and overlap no input.  Returns (dq, dk, dv), bf16."""
+    torch = _torch()
+    _rows_of(layout, q, ROWS_ALL, "full_attention_backward")
+    dev = _inputs(q, k, v)
+    B, N, H, D = q.shape
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    ts = _tok_stride(q, k, v)
+    if lse is None:
+        raise ValueError("full_attention_backward: pass the forward's lse (want_lse=True)")
+    grads = [g if g is not None else _empty((B, N, H, D), torch.bfloat16, dev, stream) for g in (dq, dk, dv)]
+    for name, t in (("dq", grads[0]), ("dk", grads[1]), ("dv", grads[2])):
+        if t.dtype is not torch.bfloat16 or t.shape != q.shape:
+            raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(q.shape)}, got {str(t.dtype)} {tuple(t.shape)}")
+    gs = _tok_stride(*grads)
+    _expect(o, (B, N, H, D), "torch.bfloat16", "o")
+    _expect(do, (B, N, H, D), "torch.bfloat16", "do")
+    _expect(lse, (B, H, N), "torch.float32", "lse")
+    _expect(dlse, (B, H, N), "torch.float32", "dlse")
+    need = layout.backward_workspace_bytes(B, H, D)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = _empty(need, torch.uint8, dev, stream, returned=False)
+    _same_device(dev, o=o, do=do, lse=lse, dlse=dlse, dq=grads[0], dk=grads[1], dv=grads[2], workspace=workspace)
+    _call(lib().rc_full_attention_backward, dev, stream, ctypes.byref(layout.c), B, H, D, scale, q.data_ptr(),
+          k.data_ptr(), v.data_ptr(), ts, o.data_ptr(), lse.data_ptr(), do.data_ptr(), _ptr(dlse), grads[0].data_ptr(),
+          grads[1].data_ptr(), grads[2].data_ptr(), gs, workspace.data_ptr(), need)
+    return tuple(grads)
 
 
 def _rows_view(t, what):

@@ -5,7 +5,7 @@
 #include <stdint.h>
 #include <string.h>
 
-#include "rc_internal.h"
+#include "rc_layer.h"
 
 namespace rc {
 namespace {
@@ -446,6 +446,56 @@ rc_status step_impl(const rc_layout* L, int32_t B, int32_t H, int32_t D, float s
 }  // namespace
 }  // namespace rc
 
+namespace rc {
+namespace {
+
+// The layer operators' launchers are weak: a build without the kernels (the
+// sanitizer build of the planner) refuses the call instead.
+template <class F>
+rc_status check_launcher(F* f, const char* what) {
+  if (f == nullptr) {
+    set_error("%s: this build has no kernels", what);
+    return RC_ERR_HIP;
+  }
+  return RC_OK;
+}
+
+// One schedule of the attention gradient from the plan of a full recompute,
+// in tiles of kBwdOwn own rows.
+rc_status plan_bwd(const rc_layout* L, BwdSched& s) {
+  Params p;
+  memset(&p, 0, sizeof p);
+  p.bm = kBwdOwn;
+  RC_TRY(plan(L, RC_ENTRY_FULL, p));
+  s.n_seg = p.n_qseg;
+  s.n_tiles = p.n_qtiles;
+  for (int i = 0; i < p.n_qseg; ++i) {
+    const QSeg& q = p.qseg[i];
+    s.seg[i] = BwdSeg{q.row0, q.len, q.tile0, q.r0, q.nr};
+  }
+  for (int i = 0; i < kMaxRanges; ++i) s.range[i] = BwdRange{p.range[i].start, p.range[i].len};
+  return RC_OK;
+}
+
+// The layout whose rows are L's keys: segment k "reads" the segments that read
+// it.
+rc_layout key_layout(const rc_layout* L) {
+  rc_layout t = *L;
+  for (int k = 0; k < L->n_seg; ++k) {
+    t.visible[k] = 0;
+    for (int q = 0; q < L->n_seg; ++q)
+      if (L->visible[q] >> k & 1u) t.visible[k] |= 1u << q;
+  }
+  return t;
+}
+
+// Per-row statistics of the gradient: two floats per (batch, head, row), each
+// in a 16-byte aligned array.
+size_t bwd_row_bytes(int64_t rows) { return (size_t(rows) * sizeof(float) + 15) & ~size_t(15); }
+
+}  // namespace
+}  // namespace rc
+
 using namespace rc;
 
 extern "C" {
@@ -709,6 +759,73 @@ rc_status rc_linear(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda,
   q.ldr = r ? ldr : 0;
   q.ldo = ldo;
   RC_TRY(hip_status(launch_linear(q, stream), "linear launch"));
+  return RC_OK;
+}
+
+size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D) {
+  if (B < 1 || H < 1 || B > 65535 || H > 65535 || (D != 64 && D != 128)) return 0;
+  if (check_layout(L, RC_ENTRY_FULL) != RC_OK) return 0;
+  return 2 * bwd_row_bytes(int64_t(B) * H * count_rows(L, RowSet::All));
+}
+
+rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, int32_t D, float scale, const void* q,
+                                     const void* k, const void* v, int64_t tok_stride, const void* o,
+                                     const float* lse, const void* d_o, const float* dlse, void* dq, void* dk,
+                                     void* dv, int64_t grad_stride, void* workspace, size_t ws_bytes, void* stream) {
+  RC_TRY(check_layout(L, RC_ENTRY_FULL));
+  RC_TRY(check_dims(B, H, D, scale));
+  RC_TRY(check_stride(tok_stride, H, D));
+  RC_TRY(check_stride(grad_stride, H, D));
+  RC_TRY(check_stride(int64_t(H) * D, H, D));  // O and dO
+  RC_TRY(check_ptr(q, "q"));
+  RC_TRY(check_ptr(k, "k"));
+  RC_TRY(check_ptr(v, "v"));
+  RC_TRY(check_ptr(o, "o"));
+  RC_TRY(check_ptr(d_o, "d_o"));
+  if (!lse) {
+    set_error("lse is null");
+    return RC_ERR_ARG;
+  }
+  RC_TRY(check_lse(lse, "lse"));
+  RC_TRY(check_lse(dlse, "dlse"));
+  RC_TRY(check_ptr(dq, "dq"));
+  RC_TRY(check_ptr(dk, "dk"));
+  RC_TRY(check_ptr(dv, "dv"));
+  const int64_t n = count_rows(L, RowSet::All), rows = int64_t(B) * H * n;
+  BwdParams p;
+  memset(&p, 0, sizeof p);
+  RC_TRY(plan_bwd(L, p.sched[0]));
+  const rc_layout t = key_layout(L);
+  RC_TRY(plan_bwd(&t, p.sched[1]));
+  RC_TRY(check_blocks(int64_t(B) * H * (p.sched[0].n_tiles + int64_t(p.sched[1].n_tiles)), "attention gradient"));
+  RC_TRY(check_blocks((rows * (D / 8) + 255) / 256, "attention gradient"));
+  const size_t need = 2 * bwd_row_bytes(rows);
+  if (!workspace || !aligned16(workspace) || ws_bytes < need) {
+    set_error("the attention gradient needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+              workspace ? ws_bytes : size_t(0));
+    return RC_ERR_WORKSPACE;
+  }
+  RC_TRY(check_launcher(launch_attention_bwd, "attention gradient"));
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.o = static_cast<const uint16_t*>(o);
+  p.d_o = static_cast<const uint16_t*>(d_o);
+  p.lse = lse;
+  p.dlse = dlse;
+  p.dq = static_cast<uint16_t*>(dq);
+  p.dk = static_cast<uint16_t*>(dk);
+  p.dv = static_cast<uint16_t*>(dv);
+  p.nlse = static_cast<float*>(workspace);
+  p.ndelta = p.nlse + bwd_row_bytes(rows) / sizeof(float);
+  p.st = tok_stride;
+  p.g_st = grad_stride;
+  p.B = B;
+  p.H = H;
+  p.n_rows = int32_t(n);
+  p.scale = scale;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  RC_TRY(hip_status(launch_attention_bwd(p, D, stream), "attention gradient launch"));
   return RC_OK;
 }
 
