@@ -12,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -19,6 +20,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librefcache.so")
 SOURCES = ["layout.cpp", "api.cpp", "attn_fwd.hip", "attn_bwd.hip", "linear.hip", "fp8_cache.hip"]
+# The attention gradient keeps its output accumulators in accumulation registers
+# by its own statements; every other matrix product of it stays in vector ones.
+SOURCE_FLAGS = {"attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 ARCH = "gfx950"
 
 
@@ -29,26 +33,38 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found: install ROCm or set HIPCC")
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Wall", "-Wno-unused-function",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           # the attention kernels read their by-value arguments at more than
-           # 300 places, beyond which LLVM would first copy them to scratch
-           "-mllvm", "-instcombine-max-copied-from-constant-users=4096",
-           "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
+def compile_command(source: str, out: str, *mode: str) -> list:
+    """The hipcc call that compiles one source (mode: -c for an object)."""
+    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
+            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+            # the attention kernels read their by-value arguments at more than
+            # 300 places, beyond which LLVM would first copy them to scratch
+            "-mllvm", "-instcombine-max-copied-from-constant-users=4096", *SOURCE_FLAGS.get(source, []),
+            "-I", INCLUDE, "-I", CSRC, *mode, os.path.join(CSRC, source), "-o", out]
+
+
+def _finish(cmd, proc, verbose: bool):
+    out = proc.communicate()[0]
+    errs = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
     if verbose:
         print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    errs = "\n".join(l for l in (res.stdout + res.stderr).splitlines()
-                     if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{errs}")
-    if verbose and errs.strip():
-        print(errs)
-    os.replace(tmp, LIB)
+        if errs.strip():
+            print(errs)
+    return f"hipcc failed ({proc.returncode}):\n{errs}" if proc.returncode != 0 else None
+
+
+def build(verbose: bool = False) -> str:
+    start = lambda cmd: subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)  # noqa: E731
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        cmds = [compile_command(s, o, "-c") for s, o in zip(SOURCES, objs)]
+        failed = [_finish(c, p, verbose) for c, p in [(c, start(c)) for c in cmds]]
+        if not any(failed):
+            link = [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", *objs, "-o", LIB + ".tmp"]
+            failed = [_finish(link, start(link), verbose)]
+    if any(failed):
+        raise RuntimeError("\n".join(f for f in failed if f))
+    os.replace(LIB + ".tmp", LIB)
     return LIB
 
 

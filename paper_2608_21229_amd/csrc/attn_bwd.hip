@@ -18,6 +18,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) const bf16x8 lds_cbf16x8;
+typedef __attribute__((address_space(3))) const f32x4 lds_cf32x4;
 
 constexpr int kTile = 64;  // streamed rows per tile
 
@@ -38,6 +40,22 @@ __device__ __forceinline__ void dma4(uint32_t lds, uint32_t voff, __amdgpu_buffe
 }
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
+// The lane index, computed where it is used: kept, it would be one more
+// register across the loop.
+__device__ __forceinline__ uint32_t fresh_lane() {
+  uint32_t l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
+// A wave-uniform 64-bit product, which the compiler computes with vector
+// instructions, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(x));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(uint64_t(x) >> 32));
+  return int64_t(uint64_t(hi) << 32 | lo);
+}
+
 template <int D, bool KV, int NB, int NW, int ST>
 struct Bwd {
   static constexpr int GR = D / 8, DC = D / 16, DB = D / 32;
@@ -47,31 +65,30 @@ struct Bwd {
   static constexpr int kOwn = 32 * NB * NW;
 };
 
-__device__ __forceinline__ int swz(int row, int gr) { return (((row & 3) << 2) | ((row >> 2) & 3)) & (gr - 1); }
+// 16-byte granule g of row r lies at slot g ^ swz(r).  16 consecutive rows at
+// one granule (128-bit reads) and 4 consecutive rows at 4 consecutive granules
+// (transpose reads) hit 16 distinct bank groups; a 128-byte row fills half of
+// the banks, so there bit 0 of the row already tells two halves apart.
+template <int D>
+__device__ __forceinline__ int swz(int row) {
+  if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  return ((row & 2) << 1) | ((row >> 1) & 2) | ((row >> 3) & 1);
+}
 
 template <int D, bool KV, int NB, int NW, int ST>
-__global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdParams p) {
+__device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const BwdSeg seg, int bh, int t) {
   using T = Bwd<D, KV, NB, NW, ST>;
+  constexpr int PF = D == 64 ? 3 : 2;  // fragments read ahead of their MFMAs
   constexpr int GR = T::GR, DC = T::DC, DB = T::DB, kT = T::kT;
-  __shared__ __attribute__((aligned(1024))) char ring[ST * T::kStage];
-  const BwdSched& sc = p.sched[KV ? 1 : 0];
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // an XCD takes a contiguous run of (batch, head, tile)
-  const int nblk = gridDim.x, bid = blockIdx.x;
-  const int xcd = bid & 7, kx = bid >> 3, per = nblk >> 3, rem = nblk & 7;
-  const int w = xcd < rem ? xcd * (per + 1) + kx : rem * (per + 1) + (xcd - rem) * per + kx;
-  const int bh = w / sc.n_tiles, t = w % sc.n_tiles;
   const int b = bh / p.H, h = bh % p.H;
-  int si = 0;
-  while (si + 1 < sc.n_seg && sc.seg[si + 1].tile0 <= t) ++si;
-  const BwdSeg seg = sc.seg[si];
-  const int own0 = (t - seg.tile0) * T::kOwn + wave * 32 * NB;  // inside the segment
+  const int own0 = t * T::kOwn + wave * 32 * NB;  // inside the segment
 
   const int64_t o_st = int64_t(p.H) * D;
-  const int64_t q_base = int64_t(b) * p.n_rows * p.st + int64_t(h) * D;
-  const int64_t o_base = int64_t(b) * p.n_rows * o_st + int64_t(h) * D;
-  const int64_t s_base = int64_t(bh) * p.n_rows;
+  const int64_t q_base = uniform(int64_t(b) * p.n_rows * p.st + int64_t(h) * D);
+  const int64_t o_base = uniform(int64_t(b) * p.n_rows * o_st + int64_t(h) * D);
+  const int64_t s_base = uniform(int64_t(bh) * p.n_rows);
   const uint16_t* x1 = (KV ? p.k : p.q) + q_base;
   const uint16_t* x2 = KV ? p.v + q_base : p.d_o + o_base;
   const int64_t x2_st = KV ? p.st : o_st;
@@ -81,7 +98,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
 
   // own operands: row lane % 32, d = 16 c + 8 hh .. +7
   bf16x8 f1[NB][DC], f2[NB][DC];
-  f32x16 cs[NB], cd[NB];  // dQ: -lse/scale and -D of the lane's query, the products' first addends
+  float cs[NB], cd[NB];  // dQ: -lse log2(e) and -D of the lane's query
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = own0 + nb * 32 + (lane & 31);
@@ -96,9 +113,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
       f2[nb][c] = e;
     }
     if constexpr (!KV) {
-      const float l = in ? p.nlse[s_base + row] : 0.f, d = in ? p.ndelta[s_base + row] : 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) cs[nb][i] = l, cd[nb][i] = d;
+      cs[nb] = in ? p.nlse[s_base + row] * p.scale_log2 : 0.f;
+      cd[nb] = in ? p.ndelta[s_base + row] : 0.f;
     }
   }
 
@@ -113,130 +129,318 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
         if constexpr (KV) acc2[nb][d][i] = 0.f;
       }
 
-  // streamed tiles
+  // Streamed tiles.  The loading cursor keeps its range in scalar registers; the
+  // range table is read again only at a range's end.
   int n_tiles = 0;
-  for (int i = 0; i < seg.nr; ++i) n_tiles += (sc.range[seg.r0 + i].len + kTile - 1) / kTile;
-  int ir = seg.r0, it = 0;  // next tile to load: range, tile in it
-  const uint32_t lds0 = lds_u32(ring);
-  const auto issue = [&](uint32_t stage) {
-    const bool any = ir < seg.r0 + seg.nr;
-    const BwdRange rg = sc.range[any ? ir : 0];
-    const int64_t row = any ? rg.start + int64_t(it) * kTile : 0;
-    const int valid = any ? min(kTile, rg.len - it * kTile) : 0;
-    const __amdgpu_buffer_rsrc_t r1 = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(y1 + row * y1_st), (short)0, __builtin_bit_cast(int, uint32_t(valid) * uint32_t(y1_st * 2)), 0x00020000);
-    const __amdgpu_buffer_rsrc_t r2 = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(y2 + row * y2_st), (short)0, __builtin_bit_cast(int, uint32_t(valid) * uint32_t(y2_st * 2)), 0x00020000);
-    constexpr int CH = kT / 1024 / NW;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int pz = (i * NW + wave) * 64 + lane, rr = pz / GR, g = (pz % GR) ^ swz(rr, GR);
-      dma16(lds0 + stage + (i * NW + wave) * 1024, uint32_t(rr) * uint32_t(y1_st * 2) + g * 16, r1);
-      dma16(lds0 + stage + kT + (i * NW + wave) * 1024, uint32_t(rr) * uint32_t(y2_st * 2) + g * 16, r2);
-    }
-    if constexpr (KV) {
-      const __amdgpu_buffer_rsrc_t rl = __builtin_amdgcn_make_buffer_rsrc(
-          (void*)((wave & 1 ? p.ndelta : p.nlse) + s_base + row), (short)0, valid * 4, 0x00020000);
-      dma4(lds0 + stage + 2 * kT + (wave & 1) * 256, lane * 4, rl);
-    }
-    if (any && ++it * kTile >= rg.len) ++ir, it = 0;
+  for (int i = 0; i < seg.nr; ++i) n_tiles += (p.range[seg.r0 + i].len + kTile - 1) / kTile;
+  int ir = seg.r0, rem = 0;
+  const uint16_t *l1 = y1, *l2 = y2;
+  const float* ls = ((wave & 1) ? p.ndelta : p.nlse) + s_base;
+  const auto load_range = [&] {
+    const BwdRange rg = p.range[ir];
+    l1 = y1 + uniform(rg.start * y1_st);
+    l2 = y2 + uniform(rg.start * y2_st);
+    ls = ((wave & 1) ? p.ndelta : p.nlse) + s_base + rg.start;
+    rem = rg.len;
   };
-  constexpr int kLoads = 2 * (kT / 1024 / NW) + (KV ? 1 : 0);
+  const auto advance = [&] {
+    rem -= kTile;
+    if (rem > 0) {
+      l1 += kTile * y1_st;
+      l2 += kTile * y2_st;
+      ls += kTile;
+    } else if (++ir < seg.r0 + seg.nr) {
+      load_range();
+    } else {
+      rem = 0;
+    }
+  };
+  if (seg.nr > 0) load_range();
+  const uint32_t lds0 = lds_u32(ring) + wave * 1024;
+  const int row_l = wave * (512 / D) + lane / GR;
+  const uint32_t gran = uint32_t((lane % GR) ^ swz<D>(row_l)) * 16;
+  const uint32_t voff1 = uint32_t(row_l) * uint32_t(y1_st * 2) + gran;
+  const uint32_t voff2 = uint32_t(row_l) * uint32_t(y2_st * 2) + gran;
+  // a wave's chunks lie a multiple of 16 rows apart, so their lane offsets are the same
+  constexpr int CH = kT / 1024 / NW, kStep = 1024 * NW / (D * 2);
+  static_assert(kStep % 16 == 0, "one swizzle for a wave's chunks");
+  constexpr int kLoads = 2 * CH + (KV ? 1 : 0);
+  // Load l of the cursor's tile; rows past the range lie beyond the record
+  // count and arrive as zeros.
+  const uint32_t step1 = uint32_t(y1_st * 2) * kStep, step2 = uint32_t(y2_st * 2) * kStep;
+  __amdgpu_buffer_rsrc_t rs1, rs2, rsl;
+  const auto rsrc = [](const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, __builtin_bit_cast(int, bytes),
+                                             0x00020000);
+  };
+  const auto start_tile = [&] {
+    const uint32_t n = min(kTile, rem);
+    rs1 = rsrc(l1, n * uint32_t(y1_st * 2));
+    rs2 = rsrc(l2, n * uint32_t(y2_st * 2));
+    if constexpr (KV) rsl = rsrc(ls, n * 4);
+  };
+  const auto issue1 = [&](uint32_t stage, int l) {
+    const int i = l / 2;
+    if (l >= 2 * CH) dma4(lds_u32(ring) + stage + 2 * kT + (wave & 1) * 256, fresh_lane() * 4, rsl);
+    else if (l & 1) dma16(lds0 + stage + kT + i * NW * 1024, voff2 + i * step2, rs2);
+    else dma16(lds0 + stage + i * NW * 1024, voff1 + i * step1, rs1);
+  };
+  const auto issue = [&](uint32_t stage) {
+    start_tile();
 #pragma unroll
-  for (int s = 0; s < ST - 1; ++s) issue(s * T::kStage);
+    for (int l = 0; l < kLoads; ++l) issue1(stage, l);
+  };
+  int valid[ST];  // rows of the tile computed and of those loaded after it
+#pragma unroll
+  for (int s = 0; s < ST - 1; ++s) {
+    valid[s] = min(kTile, rem);
+    issue(s * T::kStage);
+    advance();
+  }
 
-  // fragment addresses
+  // Fragment addresses (LDS bytes): rows lane % 32 of a sub-block, granule
+  // hh; the two transpose reads, rows 4 hh + li / 4 and 8 further.  Granule 2 c
+  // + hh and d block d are the base XOR a constant, since a stage starts at a
+  // multiple of 1 KB.
   const int li = lane & 15;
-  const uint32_t fk = (lane & 31) * D * 2 + 16 * (swz(lane & 31, GR) ^ hh);
+  const uint32_t fk = lds_u32(ring) + (lane & 31) * D * 2 + 16 * (swz<D>(lane & 31) ^ hh);
   const int gc = 2 * ((lane >> 4) & 1) + ((li & 3) >> 1);
-  const int r0 = 4 * hh + (li >> 2), r1 = r0 + 8;
-  const uint32_t v0 = r0 * D * 2 + 16 * (gc ^ swz(r0, GR)) + 8 * (li & 1);
-  const uint32_t v1 = r1 * D * 2 + 16 * (gc ^ swz(r1, GR)) + 8 * (li & 1);
-
-  int cr = seg.r0, ct = 0;
-  uint32_t cur = 0, fill = (ST - 1) * T::kStage;
-  for (int tile = 0; tile < n_tiles; ++tile) {
+  const int r0 = 4 * hh + (li >> 2);
+  const uint32_t v0 = lds_u32(ring) + r0 * D * 2 + 16 * (gc ^ swz<D>(r0)) + 8 * (li & 1);
+  constexpr uint32_t k8 = 16 * (D == 128 ? 2 : 1);  // 8 rows further the slot differs in this bit
+  const auto rd = [](uint32_t base, int c, int off) {
+    return *reinterpret_cast<lds_cbf16x8*>((base ^ uint32_t(32 * c)) + uint32_t(off));
+  };
+  const auto tr = [](uint32_t base, int f, int off) {
+    const int ks = f / DB, d = f % DB;
+    const uint32_t at = uint32_t(off + ks * 16 * D * 2);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)((base ^ uint32_t(64 * d)) + at));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)((base ^ uint32_t(64 * d) ^ k8) + at + 8 * D * 2));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  const auto rows16 = [&](uint32_t stage, int off) {  // a statistic of a sub-block's 32 rows, in accumulator order
+    const uint32_t base = lds_u32(ring) + stage + (fresh_lane() >> 5) * 16;
+    off += 2 * kT;
+    f32x16 l;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 x = *reinterpret_cast<lds_cf32x4*>(base + uint32_t(off + g * 32));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) l[4 * g + e] = x[e];
+    }
+    return l;
+  };
+  f32x16 s[NB], dp[NB];
+  f32x16 nl, nd;  // dK, dV: the rows' -lse/scale and -D, the products' first addends, read ahead
+  const auto start = [](f32x16 (&x)[NB], const f32x16& c) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[nb][r] = KV ? c[r] : 0.f;
+  };
+  const auto mm = [](bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); };
+  const auto am = [](bf16x8 a, bf16x8 b, f32x16& c) {
+    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  };
+  // Score e = 0 .. 31 of the lane: the accumulators' first halves of both
+  // blocks, then the second ones.  The argument of a score is computed one
+  // slot before its exponential.
+  float arg = 0.f;
+  const auto make_arg = [&](int e) {
+    const float x = s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)];
+    arg = KV ? x * p.scale_log2 : __builtin_fmaf(x, p.scale_log2, cs[(e >> 3) & 1]);
+    asm volatile("" : "+v"(arg));
+  };
+  const auto unit = [&](int e) {
+    float t = __builtin_amdgcn_exp2f(arg);
+    if (e < 31) make_arg(e + 1);
+    asm volatile("" : "+v"(t));  // stays in its slot
+    s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)] = t;
+  };
+  const auto units = [&](int from, int to, int slot, int slots) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e >= from && e < to && (e - from) * slots / (to - from) == slot) unit(e);
+  };
+  // dQ: scores of keys past the range are -inf (p = 0).  dK, dV need no mask:
+  // rows past the range are zeros with zero statistics, so ds = 0 and dO = 0.
+  const auto mask = [&](int valid) {
+    if (KV || valid >= 32) return;
+    const int lim = valid - 4 * hh;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + (r & 3) >= lim) s[nb][r] = -INFINITY;
+  };
+  // Exponentials of a sub-block: kE1 beside dK (dQ) of the one before, up to
+  // kE2 beside its dP, the rest beside the first half of its dV.
+  constexpr int kE1 = KV ? 11 : 16, kE2 = KV ? 24 : 32;
+  constexpr int R = PF + 1;
+  bf16x8 fr[R];
+  uint32_t cur = 0, nxt = T::kStage, fill = (ST - 1) * T::kStage;
+  if (n_tiles > 0) {  // S(0) and its first exponentials
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * kLoads) : "memory");
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
-    issue(fill);
-    const int valid = min(kTile, sc.range[cr].len - ct * kTile);
-    if (++ct * kTile >= sc.range[cr].len) ++cr, ct = 0;
-    const char* st = ring + cur;
+    if constexpr (KV) {
+      nl = rows16(0, 0);
+      nd = rows16(0, 256);
+    }
+    start(s, nl);
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      const bf16x8 a = rd(fk, c, 0);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[nb] = mm(a, f1[nb][c], s[nb]);
+    }
+    mask(valid[0]);
+    make_arg(0);
+#pragma unroll
+    for (int e = 0; e < kE1; ++e) unit(e);
+#pragma unroll
+    for (int g = 0; g < PF; ++g) fr[g] = rd(fk, g, kT);
+  }
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    uint32_t kc = fk + cur, t0 = v0 + cur;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      f32x16 s[NB], dp[NB];
-      const char* a1 = st + j * 32 * D * 2;
-      const char* a2 = a1 + kT;
-      if constexpr (KV) {
-        const char* sp = st + 2 * kT + j * 128 + hh * 16;
-        f32x16 l, d;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(sp + g * 32);
-          const f32x4 y = *reinterpret_cast<const f32x4*>(sp + 256 + g * 32);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) l[4 * g + e] = x[e], d[4 * g + e] = y[e];
-        }
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb] = l, dp[nb] = d;
-      } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb] = cs[nb], dp[nb] = cd[nb];
-      }
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(a1 + (fk ^ uint32_t(32 * c)));
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f1[nb][c], s[nb], 0, 0, 0);
-      }
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(a2 + (fk ^ uint32_t(32 * c)));
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) dp[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f2[nb][c], dp[nb], 0, 0, 0);
-      }
-      if (valid < 32 * (j + 1)) {
-        const int lim = valid - 32 * j - 4 * hh;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (8 * (r >> 2) + (r & 3) >= lim) s[nb][r] = -INFINITY;
-      }
+      // at D = 128 the registers are full: addresses are recomputed (one XOR a read), not kept
+      if constexpr (D == 128) asm volatile("" : "+v"(kc), "+v"(t0));
+      const uint32_t kn = j == 0 ? kc : fk + nxt;       // the next sub-block: rows, statistics
+      const uint32_t sn = j == 0 ? cur : nxt;
+      constexpr int kSub = 32 * D * 2;
+      const int here = j * kSub, there = j == 0 ? kSub : 0, sthere = j == 0 ? 128 : 0;
+      constexpr int GV = KV ? 2 * DB : 0;               // fragments of dV
+      constexpr int G = DC + GV + DC + 2 * DB;          // of the sub-block
+      const auto read = [&](int g) {
+        if (g < DC) return rd(kc, g, kT + here);
+        if (g < DC + GV) return tr(t0, g - DC, kT + here);
+        if (g < DC + GV + DC) return rd(kn, g - DC - GV, there);
+        if (g < G) return tr(t0, g - DC - GV - DC, here);
+        return rd(kn, g - G, kT + there);
+      };
       bf16x8 pf[NB][2], df[NB][2];
+      const auto pack = [&](int ks, int nb) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+        for (int r = 0; r < 8; ++r) pf[nb][ks][r] = (__bf16)s[nb][8 * ks + r];
+        asm volatile("" : "+v"(pf[nb][ks]));
+      };
+      const auto ds = [&](int from, int to, int slot, int slots) {  // pairs of ds = p dP
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = __builtin_amdgcn_exp2f(s[nb][r] * p.scale_log2);
-          if constexpr (KV) pf[nb][r >> 3][r & 7] = (__bf16)e;
-          df[nb][r >> 3][r & 7] = (__bf16)(e * dp[nb][r]);
-        }
+        for (int e = 0; e < 16; ++e)
+          if (e >= from && e < to && (e - from) * slots / (to - from) == slot) {
+            const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
 #pragma unroll
-      for (int f = 0; f < 2 * DB; ++f) {
-        const int ks = f / DB, d = f % DB;
-        const auto tr = [&](const char* base) {
-          const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + ks * 16 * D * 2 + (v0 ^ uint32_t(64 * d))));
-          const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + ks * 16 * D * 2 + (v1 ^ uint32_t(64 * d))));
-          return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        const bf16x8 a = tr(a1);
+            for (int i = 0; i < 2; ++i) {
+              const float x = dp[nb][8 * ks + r + i];
+              df[nb][ks][r + i] = (__bf16)(s[nb][8 * ks + r + i] * (KV ? x : x + cd[nb]));
+            }
+            asm volatile("" : "+v"(df[nb][ks]));
+          }
+      };
+      const auto next_tile = [&] {  // the next tile has landed everywhere, its stage's last readers are done
+        if (j == 0) return;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 3) * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        start_tile();
+      };
+      start(dp, nd);
+      fence();
+      int g = 0;
+      // dP(i)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          acc1[nb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, df[nb][ks], acc1[nb][d], 0, 0, 0);
-        if constexpr (KV) {
-          const bf16x8 e = tr(a2);
+      for (int c = 0; c < DC; ++c, ++g) {
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            acc2[nb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e, pf[nb][ks], acc2[nb][d], 0, 0, 0);
+        for (int nb = 0; nb < NB; ++nb) {
+          dp[nb] = mm(fr[g % R], f2[nb][c], dp[nb]);
+          if (!KV && nb == 0 && g + PF == DC) next_tile();  // before the first read of S(i + 1)'s rows
+          if (nb == 0) fr[(g + PF) % R] = read(g + PF);
+          units(kE1, kE2, 2 * c + nb, 2 * DC);
+          if (KV && 2 * c + nb >= 2 * DC - 4 && nb == 0) pack(0, c - (DC - 2));
+          fence();
         }
       }
+      if constexpr (KV) {
+        next_tile();  // S(i + 1)'s rows are read from dV on
+        fence();
+        // dV(i)
+#pragma unroll
+        for (int f = 0; f < 2 * DB; ++f, ++g) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            am(fr[g % R], pf[nb][f / DB], acc2[nb][f % DB]);
+            if (nb == 0) fr[(g + PF) % R] = read(g + PF);
+            if (f < DB) units(kE2, 32, 2 * f + nb, 2 * DB);
+            else ds(0, 8, 2 * (f - DB) + nb, 2 * DB);
+            if (f == DB - 1) pack(1, nb);
+            if (f == 2 * DB - 1 && nb == 0) nl = rows16(sn, sthere);
+            fence();
+          }
+        }
+      }
+      // S(i + 1)
+      f32x16 s2[NB];
+      start(s2, nl);
+#pragma unroll
+      for (int c = 0; c < DC; ++c, ++g) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          s2[nb] = mm(fr[g % R], f1[nb][c], s2[nb]);
+          if (nb == 0) fr[(g + PF) % R] = read(g + PF);
+          if (KV) ds(8, 16, 2 * c + nb, DC);
+          else ds(0, 16, 2 * c + nb - 2, 2 * DC - 2);
+          fence();
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[nb] = s2[nb];
+      if (j == 1) {
+        valid[ST - 1] = min(kTile, rem);
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) valid[s] = valid[s + 1];
+      }
+      mask(j == 0 ? valid[0] - 32 : valid[0]);
+      fence();
+      // dK(i) or dQ(i)
+#pragma unroll
+      for (int f = 0; f < 2 * DB; ++f, ++g) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          am(fr[g % R], df[nb][f / DB], acc1[nb][f % DB]);
+          if (nb == 0) fr[(g + PF) % R] = read(g + PF);
+          if (KV && f == 2 * DB - 2 && nb == 0) nd = rows16(sn, sthere + 256);
+          if (f == 0 && nb == 1) make_arg(0);
+          units(0, kE1, 2 * f + nb - 2, 4 * DB - 2);
+          if (j == 1)
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+              if (l * (4 * DB) / kLoads == 2 * f + nb) issue1(fill, l);
+          fence();
+        }
+      }
+      bf16x8 first[PF];  // the next sub-block's first fragments
+#pragma unroll
+      for (int i = 0; i < PF; ++i) first[i] = fr[(G + i) % R];
+#pragma unroll
+      for (int i = 0; i < PF; ++i) fr[i] = first[i];
     }
-    cur = cur + T::kStage == ST * T::kStage ? 0 : cur + T::kStage;
+    advance();
+    cur = nxt;
+    nxt = nxt + T::kStage == ST * T::kStage ? 0 : nxt + T::kStage;
     fill = fill + T::kStage == ST * T::kStage ? 0 : fill + T::kStage;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the work-group
+
+  // The compiler does not see that the accumulators come from MFMAs: the last
+  // of them are waited for here, before the first read.
+  const auto settle = [](f32x16& c) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(c)); };
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      settle(acc1[nb][d]);
+      if constexpr (KV) settle(acc2[nb][d]);
+    }
 
   const auto store = [&](uint16_t* out, const f32x16& acc, int nb, int d, float f) {
     const int r = own0 + nb * 32 + (lane & 31);
@@ -264,6 +468,27 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
     }
 }
 
+template <int D, int NB, int NW, int ST>
+__global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdParams p) {
+  __shared__ __attribute__((aligned(1024))) char ring[ST * Bwd<D, true, NB, NW, ST>::kStage];
+  // The hardware deals work-groups round-robin to the 8 XCDs.  Where the heads
+  // divide over them, an XCD takes whole heads, whose streamed rows then share
+  // its L2 (two 1024-pixel samples of 24 heads: 4.10 ms, and 4.19 without).
+  // Work-groups run in order of their segment (longest first), then batch and
+  // head, then tile.
+  const int bhs = p.B * p.H;
+  const bool split = bhs % 8 == 0;
+  const int hx = split ? bhs / 8 : bhs;
+  const int w = split ? blockIdx.x >> 3 : blockIdx.x;
+  int si = 0;
+  while (si + 1 < p.n_seg && p.seg[si + 1].tile0 * hx <= w) ++si;
+  const BwdSeg seg = p.seg[si];
+  const int in_seg = w - seg.tile0 * hx, seg_tiles = (seg.len + kBwdOwn - 1) / kBwdOwn;
+  const int bh = (split ? (blockIdx.x & 7) * hx : 0) + in_seg / seg_tiles, t = in_seg % seg_tiles;
+  if (seg.keys) bwd_tile<D, true, NB, NW, ST>(p, ring, seg, bh, t);
+  else bwd_tile<D, false, NB, NW, ST>(p, ring, seg, bh, t);
+}
+
 // -lse / scale and -D of every row; rows that read nothing get -inf and 0.
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_rows_kernel(const BwdParams p) {
@@ -288,17 +513,14 @@ __global__ __launch_bounds__(256) void attn_bwd_rows_kernel(const BwdParams p) {
   p.ndelta[at] = none ? 0.f : (p.dlse ? p.dlse[at] : 0.f) - s;
 }
 
-#ifndef BWD_NB
-#define BWD_NB 1
-#endif
 template <int D>
 void launch(const BwdParams& p, hipStream_t s) {
   const int64_t rows = int64_t(p.B) * p.n_rows * p.H;
   hipLaunchKernelGGL(attn_bwd_rows_kernel<D>, dim3((rows * (D / 8) + 255) / 256), dim3(256), 0, s, p);
   const int64_t bh = int64_t(p.B) * p.H;
-  constexpr int NB = BWD_NB, NW = kBwdOwn / 32 / NB, ST = 3;
-  hipLaunchKernelGGL((attn_bwd_kernel<D, true, NB, NW, ST>), dim3(bh * p.sched[1].n_tiles), dim3(64 * NW), 0, s, p);
-  hipLaunchKernelGGL((attn_bwd_kernel<D, false, NB, NW, ST>), dim3(bh * p.sched[0].n_tiles), dim3(64 * NW), 0, s, p);
+  constexpr int NB = 2, NW = kBwdOwn / 32 / NB, ST = 3;
+  hipLaunchKernelGGL((attn_bwd_kernel<D, NB, NW, ST>), dim3(bh * p.n_tiles),
+                     dim3(64 * NW), 0, s, p);
 }
 
 }  // namespace

@@ -13,21 +13,17 @@
 namespace rc {
 
 // ---------------------------------------------------------------- attention gradient
-// One pass over the visible (query, key) pairs per schedule.  `own` rows stay
-// with a work-group (queries for dQ, keys for dK and dV), the rows they meet
-// are streamed.
+// Two kinds of work-groups pass over the visible (query, key) pairs: those that
+// hold queries sum dQ, those that hold keys sum dK and dV.  The rows a
+// work-group holds are its own, the rows they meet are streamed.
 struct BwdSeg {
   int32_t row0, len;  // own rows
-  int32_t tile0;      // first own tile
+  int32_t tile0;      // first own tile, over the segments of both kinds in launch order
   int32_t r0, nr;     // streamed ranges
+  int32_t keys;       // own rows are keys
 };
 struct BwdRange {
   int32_t start, len;
-};
-struct BwdSched {
-  int32_t n_seg, n_tiles;
-  BwdSeg seg[RC_MAX_SEGMENTS];
-  BwdRange range[kMaxRanges];
 };
 constexpr int kBwdOwn = 256;  // own rows of a tile
 
@@ -47,7 +43,9 @@ struct BwdParams {
   int64_t st, g_st;    // token strides (elements) of Q/K/V and of the gradients; batch stride N times that
   int32_t B, H, n_rows;
   float scale, scale_log2;
-  BwdSched sched[2];   // own = queries (dQ), own = keys (dK, dV)
+  int32_t n_seg, n_tiles;
+  BwdSeg seg[2 * RC_MAX_SEGMENTS];
+  BwdRange range[2 * kMaxRanges];
 };
 int launch_attention_bwd(const BwdParams& p, int D, void* stream) RC_WEAK;
 

@@ -159,6 +159,17 @@ def test_batch_entries_and_repeats_are_the_same_bits():
             assert torch.equal(a[at], c)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("preset", ["perref", "paper"])
+def test_many_work_groups(preset, D):
+    """More work-groups than CUs, whose rings wrap many times: against the formula, and the same bits in every pass."""
+    L = rc.Layout([(0, 37), (1, 203), (2, 1577), (3, 1024), (3, 519)], preset)
+    (q, k, v, o, lse, do, dl), got = _check(L, 1, 24, D, seed=31, fused=True, dlse=True)
+    for _ in range(4):
+        for a, b in zip(rc.full_attention_backward(L, q, k, v, o, lse, do, dlse=dl), got):
+            assert torch.equal(a, b)
+
+
 def test_finite_differences():
     """sum(w O) + sum(u lse) along random directions, in 64 bits, against the kernel's gradient of them."""
     L = rc.Layout([(0, 5), (1, 40), (2, 70), (3, 33)], "paper")
