@@ -355,6 +355,107 @@ rc_status rc_step_masked_attention_fp8(const rc_layout* L, int32_t B, int32_t H,
 rc_status rc_linear(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const void* w,
                     const void* r, int64_t ldr, void* out, int64_t ldo, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The parts of a layer between the projections and the attention: rotation
+ * of queries and keys by position, and the gated norm between blocks, each
+ * with its gradient. */
+
+#define RC_MAX_ROTARY_AXES 8
+
+/* How a head row's channels rotate.  `axes` widths (even, at least 0) add up
+ * to the rotated width R <= head_dim; pair p = 0 .. R/2 - 1 belongs to the
+ * axis whose width it falls into and turns by position[axis] * frequency(p),
+ * the channels past R stay.
+ *   interleaved  1: pair p is channels 2p, 2p + 1
+ *                0: pair p is channels p, p + R/2 (R a multiple of 16)
+ *   continuous   0: each axis of width d has frequencies theta^(-2 i / d), i = 0 ..
+ *                1: one ladder theta^(-2 p / R) over all axes
+ * Filled by rc_rotary_init and read only during calls. */
+typedef struct {
+  int32_t head_dim, n_axes, width, interleaved;
+  uint8_t axis[64];
+  double turns[64];  /* revolutions per unit of position */
+} rc_rotary;
+rc_status rc_rotary_init(rc_rotary* R, int32_t head_dim, int32_t n_axes, const int32_t* axes, double theta,
+                         int32_t interleaved, int32_t continuous);
+
+/* Queries and keys: RMS norm over each head row (where a weight is given),
+ * then the rotation.
+ *   z = x * rsqrt(mean(x^2) + eps) * norm;  out = rotated z, rounded once
+ *   q, k          [B, N, H, D] bf16 with D contiguous, head stride D, token stride
+ *                 tok_stride, as for the attention; either may be NULL
+ *   positions     [N, n_axes], or with pos_batch = 1 [B, N, n_axes], contiguous:
+ *                 int32, or fp32 with pos_float = 1.  Angles are reduced in 64 bits.
+ *   q_norm, k_norm  [D] bf16, NULL: no norm
+ *   q_out, k_out  as q and k, token stride out_stride; each may be its input (same
+ *                 stride), otherwise they overlap nothing
+ * B * N < 2^31.  N = 0 is a no-op.  RC_ERR_UNSUPPORTED for head_dim other than 64/128. */
+rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* q, const void* k,
+                       int64_t tok_stride, const void* positions, int32_t pos_float, int32_t pos_batch,
+                       const void* q_norm, const void* k_norm, float eps, void* q_out, void* k_out,
+                       int64_t out_stride, void* stream);
+
+/* Its gradient: dq_in, dk_in from the gradients dq, dk of the outputs.
+ *   q, k          the forward's inputs (token stride tok_stride); read only where a norm is
+ *   dq_norm, dk_norm  [D] fp32 out: the norms' gradients; NULL where there is no norm
+ *   dq, dk        token stride grad_stride;  dq_in, dk_in: token stride out_stride, each may be its gradient input
+ *   workspace     rc_rotary_backward_workspace_bytes bytes (16-byte aligned) with a norm, else NULL */
+rc_status rc_qk_rotary_backward(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* dq, const void* dk,
+                                int64_t grad_stride, const void* positions, int32_t pos_float, int32_t pos_batch,
+                                const void* q, const void* k, int64_t tok_stride, const void* q_norm,
+                                const void* k_norm, float eps, void* dq_in, void* dk_in, int64_t out_stride,
+                                float* dq_norm, float* dk_norm, void* workspace, size_t ws_bytes, void* stream);
+size_t rc_rotary_backward_workspace_bytes(const rc_rotary* R, int32_t B, int64_t N);
+
+#define RC_NORM_LAYER 0  /* mean removed, no affine */
+#define RC_NORM_RMS 1
+
+/* Gated norm between two blocks of a layer, rows of C channels:
+ *   u  = x, or with post = 1  x * rsqrt(mean(x^2) + eps) * post_weight
+ *   h' = h + residual_scale * gate * u
+ *   y  = norm(h') * weight * (1 + scale) + shift
+ * gate, scale and shift hold one vector per batch entry and group; span s gives
+ * rows[s] consecutive rows of each batch entry to group[s] (live rows are
+ * modulated by the timestep, static ones by timestep 0).  The spans' rows add
+ * up to N; groups are 0 .. n_groups - 1. */
+typedef struct {
+  int32_t B, C, n_groups, norm, post;
+  int64_t N;                     /* rows per batch entry, B * N < 2^31 */
+  float eps, residual_scale;
+  int64_t mod_batch, mod_group;  /* element strides of gate, scale, shift: batch entry, group */
+  int32_t n_spans;
+  int32_t rows[RC_MAX_SEGMENTS], group[RC_MAX_SEGMENTS];
+} rc_norm;
+
+/* Rows are bf16 [B, N, C] with C contiguous, row stride ld* (elements, >= C, a
+ * multiple of 8, <= 2^22) and batch stride N * ld*; C a multiple of 8 up to
+ * 16384; pointers 16-byte aligned; mod strides multiples of 8, >= 0.
+ *   x             NULL: no residual; then h' = h and h_out is NULL
+ *   gate, scale, shift, weight [C], post_weight [C]  bf16, each may be NULL (ones; shift: zeros)
+ *   h_out         h' rounded; may be h (same stride).  y is computed from h' before its rounding
+ *   y             NULL: only the residual
+ * Outputs overlap no input except as said.  N = 0 is a no-op. */
+rc_status rc_gated_norm(const rc_norm* d, const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,
+                        const void* scale, const void* shift, const void* weight, const void* post_weight,
+                        void* h_out, int64_t ldho, void* y, int64_t ldy, void* stream);
+
+/* Its gradient, taken at the rows h = h' after the residual.
+ *   dy            the gradient of y, NULL: none (then scale, shift, weight and their gradients are NULL)
+ *   dh            the gradient of h' from elsewhere, NULL: none
+ *   dh_in         out: the gradient of the forward's h;  dx out: of x (NULL without x)
+ *                 dh_in may be dh or dy, dx may be x (same strides)
+ *   dgate, dscale, dshift  [B, n_groups, C] fp32 out, contiguous; dweight, dpost_weight [C] fp32
+ *                 out; each may be NULL.  Groups without rows get zeros.
+ *   workspace     rc_gated_norm_backward_workspace_bytes bytes, 16-byte aligned
+ * Deterministic: the sums over rows keep one order. */
+rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy, const void* dh, int64_t lddh,
+                                 const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,
+                                 const void* scale, const void* weight, const void* post_weight, void* dh_in,
+                                 int64_t lddhi, void* dx, int64_t lddx, float* dgate, float* dscale, float* dshift,
+                                 float* dweight, float* dpost_weight, void* workspace, size_t ws_bytes,
+                                 void* stream);
+size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);
+
 /* Bytes of the static device array (per GPU) behind
  * rc_step_masked_attention_noalloc: 128 MiB, enough for the balanced schedule
  * at D = 128 (65 MiB) and for two splits over 24 heads x 4608 live rows. */

@@ -11,7 +11,7 @@ residual) through it.
 """
 from .binding import (  # noqa: F401
     Layout, RcError, lib, ref_kv_prefill, step_masked_attention, step_masked_attention_noalloc, full_attention,
-    full_attention_backward,
+    full_attention_backward, Rotary, qk_rotary, qk_rotary_backward, gated_norm, gated_norm_backward, NormGrads,
     linear, NOALLOC_SCRATCH_BYTES,
     ref_kv_prefill_fp8, step_masked_attention_fp8, fp8_cache_shapes,
     SEG_ANCHOR, SEG_TEXT, SEG_TARGET, SEG_REF,

@@ -14,6 +14,7 @@ Loading fails loudly if the library has not been built
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import math
 import os
@@ -53,9 +54,23 @@ class rc_layout(ctypes.Structure):
                 ("visible", ctypes.c_uint32 * RC_MAX_SEGMENTS)]
 
 
+class rc_rotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64), ("turns", ctypes.c_double * 64)]
+
+
+class rc_norm(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("C", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("N", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("mod_batch", ctypes.c_int64), ("mod_group", ctypes.c_int64),
+                ("n_spans", ctypes.c_int32), ("rows", ctypes.c_int32 * RC_MAX_SEGMENTS),
+                ("group", ctypes.c_int32 * RC_MAX_SEGMENTS)]
+
+
 _LIB = None
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
-_PL = ctypes.POINTER(rc_layout)
+_f64 = ctypes.c_double
+_PL, _PR, _PN = ctypes.POINTER(rc_layout), ctypes.POINTER(rc_rotary), ctypes.POINTER(rc_norm)
 SIGNATURES = {
     "rc_layout_preset": (_i32, [_PL, _i32]),
     "rc_layout_validate": (_i32, [_PL, _i32]),
@@ -84,6 +99,16 @@ SIGNATURES = {
     "rc_full_backward_workspace_bytes": (_sz, [_PL, _i32, _i32, _i32]),
     "rc_full_attention_backward": (_i32, [_PL, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
                                           _vp, _vp, _i64, _vp, _sz, _vp]),
+    "rc_rotary_init": (_i32, [_PR, _i32, _i32, ctypes.POINTER(_i32), _f64, _i32, _i32]),
+    "rc_qk_rotary": (_i32, [_PR, _i32, _i64, _i32, _vp, _vp, _i64, _vp, _i32, _i32, _vp, _vp, _f32, _vp, _vp, _i64,
+                            _vp]),
+    "rc_rotary_backward_workspace_bytes": (_sz, [_PR, _i32, _i64]),
+    "rc_qk_rotary_backward": (_i32, [_PR, _i32, _i64, _i32, _vp, _vp, _i64, _vp, _i32, _i32, _vp, _vp, _i64, _vp, _vp,
+                                     _f32, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "rc_gated_norm": (_i32, [_PN, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "rc_gated_norm_backward_workspace_bytes": (_sz, [_PN]),
+    "rc_gated_norm_backward": (_i32, [_PN, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64,
+                                      _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "rc_status_string": (ctypes.c_char_p, [_i32]),
     "rc_last_error": (ctypes.c_char_p, []),
 }
@@ -189,6 +214,16 @@ class Layout:
         _check(lib().rc_prefill_launch_plan(ctypes.byref(self.c), B, H, D, ctypes.byref(a), ctypes.byref(c),
                                             ctypes.byref(r)))
         return a.value, c.value, r.value
+
+    def modulation_spans(self, which: int = ROWS_ALL, live: int = 0, static: int = 1):
+        """(rows, group) spans of a row class for gated_norm: live segments
+        (text, target) take group `live`, static ones (anchors, references) `static`."""
+        spans = []
+        for k, n in self.segments:
+            is_live = k in (SEG_TEXT, SEG_TARGET)
+            if which == ROWS_ALL or (which == ROWS_LIVE) == is_live:
+                spans.append((n, live if is_live else static))
+        return spans
 
     def auto_splits(self, B: int, H: int, D: int) -> int:
         return int(lib().rc_step_auto_splits(ctypes.byref(self.c), B, H, D))
@@ -481,6 +516,263 @@ def linear(a, w, residual=None, out=None, stream=None):
     _call(lib().rc_linear, dev, stream, M, N, K, a.data_ptr(), lda, w.data_ptr(), _ptr(residual), ldr, out.data_ptr(),
           ldo)
     return out
+
+
+# ---------------------------------------------------------------- rotation of queries and keys
+class Rotary:
+    """How a head row's channels turn with the token's position (rc_rotary).
+
+    axes: rotated widths per position axis, e.g. (16, 56, 56) for (time,
+    height, width) of 128-wide heads; channels past their sum stay.
+    interleaved: pairs of neighbouring channels, else of the rotated width's
+    two halves.  continuous: one frequency ladder over all axes, else each
+    axis has its own from 1 down to 1 / theta."""
+
+    def __init__(self, head_dim: int, axes: Sequence[int], theta: float = 10000.0, interleaved: bool = True,
+                 continuous: bool = False):
+        self.c = rc_rotary()
+        self.head_dim, self.axes = int(head_dim), tuple(int(a) for a in axes)
+        arr = (ctypes.c_int32 * max(1, len(self.axes)))(*self.axes)
+        _check(lib().rc_rotary_init(ctypes.byref(self.c), self.head_dim, len(self.axes), arr, float(theta),
+                                    int(interleaved), int(continuous)))
+
+
+def _heads(name, t, like=None, D=None):
+    """A bf16 [B, N, H, D] GPU tensor, of like's shape and device."""
+    if t.dim() != 4 or t.dtype is not _torch().bfloat16 or not t.is_cuda or (D is not None and t.shape[3] != D):
+        raise ValueError(f"{name} must be a bf16 [B, N, H, {D or 'D'}] GPU tensor, got {str(t.dtype)} "
+                         f"{tuple(t.shape)} on {t.device}")
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError(f"{name} must have shape {tuple(like.shape)} on {like.device}, got {tuple(t.shape)} on {t.device}")
+
+
+def _given(*ts):
+    return [t for t in ts if t is not None]
+
+
+def _positions(rotary: Rotary, t, positions):
+    """(is fp32, has a batch axis) of the positions of t's tokens."""
+    torch = _torch()
+    B, N, A = t.shape[0], t.shape[1], len(rotary.axes)
+    if positions.dtype not in (torch.int32, torch.float32) or not positions.is_contiguous():
+        raise ValueError(f"positions must be contiguous int32 or float32, got {str(positions.dtype)}")
+    if tuple(positions.shape) not in ((N, A), (B, N, A)):
+        raise ValueError(f"positions must be {(N, A)} or {(B, N, A)}, got {tuple(positions.shape)}")
+    return int(positions.dtype is torch.float32), int(positions.dim() == 3)
+
+
+def _norm_weight(name, w, D):
+    if w is not None and (w.dtype is not _torch().bfloat16 or tuple(w.shape) != (D,) or not w.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous bf16 [{D}] tensor, got {str(w.dtype)} {tuple(w.shape)}")
+
+
+def _outputs(outs, ins, names, dev, stream):
+    """An output per input (None where there is none), and their token stride."""
+    outs = [None if i is None else _empty(tuple(i.shape), i.dtype, dev, stream) if o is None else o
+            for o, i in zip(outs, ins)]
+    for n, o, i in zip(names, outs, ins):
+        if o is not None:
+            _heads(n, o, i)
+    return outs, _tok_stride(*_given(*outs))
+
+
+def qk_rotary(rotary: Rotary, q, k, positions, q_norm=None, k_norm=None, eps: float = 1e-6, q_out=None, k_out=None,
+              stream=None):
+    """RMS norm (where a weight is given) and rotation of queries and keys.
+    q, k: [B, N, H, D] bf16 views with one token stride, either may be None;
+    positions: [N, axes] or [B, N, axes], int32 or float32; q_norm, k_norm:
+    [D] bf16.  q_out may be q and k_out k (in place).  Returns (q_out, k_out)."""
+    given = _given(q, k)
+    if not given:
+        raise ValueError("qk_rotary: pass q, k or both")
+    for name, t in (("q", q), ("k", k)):
+        if t is not None:
+            _heads(name, t, given[0], rotary.head_dim)
+    B, N, H, D = given[0].shape
+    dev = given[0].device
+    pf, pb = _positions(rotary, given[0], positions)
+    _norm_weight("q_norm", q_norm, D)
+    _norm_weight("k_norm", k_norm, D)
+    ts = _tok_stride(*given)
+    (qo, ko), os_ = _outputs((q_out, k_out), (q, k), ("q_out", "k_out"), dev, stream)
+    _same_device(dev, positions=positions, q_norm=q_norm, k_norm=k_norm)
+    _call(lib().rc_qk_rotary, dev, stream, ctypes.byref(rotary.c), B, N, H, _ptr(q), _ptr(k), ts, positions.data_ptr(),
+          pf, pb, _ptr(q_norm), _ptr(k_norm), eps, _ptr(qo), _ptr(ko), os_)
+    return qo, ko
+
+
+def qk_rotary_backward(rotary: Rotary, dq, dk, positions, q=None, k=None, q_norm=None, k_norm=None, eps: float = 1e-6,
+                       dq_out=None, dk_out=None, workspace=None, stream=None):
+    """Gradient of qk_rotary: dq, dk are the gradients of its outputs; q, k its
+    inputs, needed where there is a norm.  dq_out may be dq and dk_out dk.
+    Returns (dq_out, dk_out, dq_norm, dk_norm); the norms' gradients are [D] fp32."""
+    torch = _torch()
+    given = _given(dq, dk)
+    if not given:
+        raise ValueError("qk_rotary_backward: pass dq, dk or both")
+    for name, t in (("dq", dq), ("dk", dk)):
+        if t is not None:
+            _heads(name, t, given[0], rotary.head_dim)
+    B, N, H, D = given[0].shape
+    dev = given[0].device
+    pf, pb = _positions(rotary, given[0], positions)
+    _norm_weight("q_norm", q_norm, D)
+    _norm_weight("k_norm", k_norm, D)
+    inputs = []
+    for name, w, t, g in (("q", q_norm, q, dq), ("k", k_norm, k, dk)):
+        if w is not None:
+            if t is None or g is None:
+                raise ValueError(f"{name}_norm needs {name} and d{name}")
+            _heads(name, t, g)
+            inputs.append(t)
+    ts = _tok_stride(*inputs) if inputs else 0
+    gs = _tok_stride(*given)
+    (qo, ko), os_ = _outputs((dq_out, dk_out), (dq, dk), ("dq_out", "dk_out"), dev, stream)
+    dw = [_empty((D,), torch.float32, dev, stream) if w is not None else None for w in (q_norm, k_norm)]
+    need = int(lib().rc_rotary_backward_workspace_bytes(ctypes.byref(rotary.c), B, N)) if inputs else 0
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = _empty(need, torch.uint8, dev, stream, returned=False)
+    _same_device(dev, positions=positions, q_norm=q_norm, k_norm=k_norm, workspace=workspace if need else None)
+    _call(lib().rc_qk_rotary_backward, dev, stream, ctypes.byref(rotary.c), B, N, H, _ptr(dq), _ptr(dk), gs,
+          positions.data_ptr(), pf, pb, _ptr(q if q_norm is not None else None), _ptr(k if k_norm is not None else None),
+          ts, _ptr(q_norm), _ptr(k_norm), eps, _ptr(qo), _ptr(ko), os_, _ptr(dw[0]), _ptr(dw[1]),
+          _ptr(workspace) if need else None, need)
+    return qo, ko, dw[0], dw[1]
+
+
+# ---------------------------------------------------------------- gated norm between blocks
+NORMS = {"layer": 0, "rms": 1}
+NormGrads = collections.namedtuple("NormGrads", "h x gate scale shift weight post_weight")
+
+
+def _row_stride(name, t, like=None):
+    """Row stride of a bf16 [B, N, C] GPU tensor with C contiguous and batch stride N row strides."""
+    if t.dim() != 3 or t.dtype is not _torch().bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name} must be a bf16 [B, N, C] GPU tensor, got {str(t.dtype)} {tuple(t.shape)} on {t.device}")
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError(f"{name} must have shape {tuple(like.shape)} on {like.device}, got {tuple(t.shape)} on {t.device}")
+    B, N, C = t.shape
+    sb, sn, sc = t.stride()
+    if C > 1 and sc != 1:
+        raise ValueError(f"{name} must have unit channel stride")
+    if N <= 1:
+        return sb if N == 1 and B > 1 else C
+    if B > 1 and sb != N * sn:
+        raise ValueError(f"{name} must have batch stride N * row stride")
+    return sn
+
+
+def _norm_desc(h, spans, norm, post, eps, residual_scale, mods, weight, post_weight):
+    """rc_norm of a call: shapes, spans and the strides that gate, scale and shift share."""
+    torch = _torch()
+    B, N, C = h.shape
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {sorted(NORMS)}, got {norm!r}")
+    spans = [(N, 0)] if spans is None else spans
+    if len(spans) > RC_MAX_SEGMENTS:
+        raise ValueError(f"at most {RC_MAX_SEGMENTS} spans")
+    d = rc_norm(B=B, C=C, norm=NORMS[norm], post=int(post), N=N, eps=eps, residual_scale=residual_scale,
+                n_spans=len(spans))
+    top = 0
+    for i, (n, g) in enumerate(spans):
+        d.rows[i], d.group[i] = n, g
+        top = max(top, g)
+    G, strides = top + 1, None
+    for name, t in mods:
+        if t is None:
+            continue
+        if t.dim() != 3 or t.dtype is not torch.bfloat16 or t.shape[0] != B or t.shape[2] != C or t.device != h.device:
+            raise ValueError(f"{name} must be a bf16 [{B}, groups, {C}] tensor on {h.device}, got {str(t.dtype)} "
+                             f"{tuple(t.shape)} on {t.device}")
+        if C > 1 and t.stride(2) != 1:
+            raise ValueError(f"{name} must have unit channel stride")
+        mine = (t.shape[1], t.stride(0) if B > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+        if strides is not None and mine != strides:
+            raise ValueError("gate, scale and shift must share groups and strides (chunks of one tensor do)")
+        strides = mine
+    if strides is not None:
+        G, d.mod_batch, d.mod_group = strides
+    d.n_groups = G
+    for name, w in (("weight", weight), ("post_weight", post_weight)):
+        _norm_weight(name, w, C)
+    _same_device(h.device, weight=weight, post_weight=post_weight)
+    return d, G
+
+
+def gated_norm(h, x=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, norm: str = "layer",
+               post_norm: bool = False, spans=None, residual_scale: float = 1.0, eps: float = 1e-6, h_out=None, y=None,
+               want_y: bool = True, stream=None):
+    """h' = h + residual_scale * gate * u, with u = x or (post_norm, implied by
+    post_weight) the RMS norm of x, and y = norm(h') * weight * (1 + scale) + shift.
+
+    h, x: [B, N, C] bf16 rows; gate, scale, shift: [B, groups, C] (chunks of
+    one modulation tensor work); weight, post_weight: [C]; spans: (rows,
+    group) pairs over N, e.g. Layout.modulation_spans (None: one group).
+    Returns (h', y); h_out may be h.  Without x, h' is h itself; want_y=False
+    computes the residual alone."""
+    torch = _torch()
+    ldh = _row_stride("h", h)
+    dev = h.device
+    post = post_norm or post_weight is not None
+    d, _ = _norm_desc(h, spans, norm, post, eps, residual_scale, (("gate", gate), ("scale", scale), ("shift", shift)),
+                      weight, post_weight)
+    ldx = ldo = ldy = 0
+    if x is not None:
+        ldx = _row_stride("x", x, h)
+        if h_out is None:
+            h_out = _empty(tuple(h.shape), torch.bfloat16, dev, stream)
+        ldo = _row_stride("h_out", h_out, h)
+    elif h_out is not None:
+        raise ValueError("h_out is written only with x")
+    if want_y:
+        if y is None:
+            y = _empty(tuple(h.shape), torch.bfloat16, dev, stream)
+        ldy = _row_stride("y", y, h)
+    elif y is not None:
+        raise ValueError("y is written only with want_y")
+    _call(lib().rc_gated_norm, dev, stream, ctypes.byref(d), h.data_ptr(), ldh, _ptr(x), ldx, _ptr(gate), _ptr(scale),
+          _ptr(shift), _ptr(weight), _ptr(post_weight), _ptr(h_out), ldo, _ptr(y), ldy)
+    return (h if x is None else h_out), y
+
+
+def gated_norm_backward(dy, h, x=None, dh=None, gate=None, scale=None, shift=None, weight=None, post_weight=None,
+                        norm: str = "layer", post_norm: bool = False, spans=None, residual_scale: float = 1.0,
+                        eps: float = 1e-6, dh_out=None, dx=None, workspace=None, stream=None):
+    """Gradient of gated_norm at its output rows h (= h').  dy: the gradient of
+    y (None: none); dh: the gradient of h' from elsewhere (None: none); the
+    other arguments as the forward's.  dh_out may be dh or dy, dx may be x.
+    Returns NormGrads(h, x, gate, scale, shift, weight, post_weight): the rows'
+    in bf16, the shared ones in fp32 ([B, groups, C] and [C]), None where the
+    forward had none."""
+    torch = _torch()
+    ldh = _row_stride("h", h)
+    dev = h.device
+    post = post_norm or post_weight is not None
+    d, G = _norm_desc(h, spans, norm, post, eps, residual_scale, (("gate", gate), ("scale", scale), ("shift", shift)),
+                      weight, post_weight)
+    B, _, C = h.shape
+    lddy = _row_stride("dy", dy, h) if dy is not None else 0
+    lddh = _row_stride("dh", dh, h) if dh is not None else 0
+    ldx = _row_stride("x", x, h) if x is not None else 0
+    dh_out = _empty(tuple(h.shape), torch.bfloat16, dev, stream) if dh_out is None else dh_out
+    ldo = _row_stride("dh_out", dh_out, h)
+    lddx = 0
+    if x is not None:
+        dx = _empty(tuple(h.shape), torch.bfloat16, dev, stream) if dx is None else dx
+        lddx = _row_stride("dx", dx, h)
+    elif dx is not None:
+        raise ValueError("dx is written only with x")
+    like = lambda t, shape: None if t is None else _empty(shape, torch.float32, dev, stream)  # noqa: E731
+    dgate, dscale, dshift = (like(t, (B, G, C)) for t in (gate, scale, shift))
+    dweight, dpost = like(weight, (C,)), like(post_weight, (C,))
+    need = int(lib().rc_gated_norm_backward_workspace_bytes(ctypes.byref(d)))
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = _empty(need, torch.uint8, dev, stream, returned=False)
+    _same_device(dev, workspace=workspace if need else None)
+    _call(lib().rc_gated_norm_backward, dev, stream, ctypes.byref(d), _ptr(dy), lddy, _ptr(dh), lddh, h.data_ptr(), ldh,
+          _ptr(x), ldx, _ptr(gate), _ptr(scale), _ptr(weight), _ptr(post_weight), dh_out.data_ptr(), ldo, _ptr(dx), lddx,
+          _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dweight), _ptr(dpost), _ptr(workspace) if need else None, need)
+    return NormGrads(dh_out, dx, dgate, dscale, dshift, dweight, dpost)
 
 
 # ---------------------------------------------------------------- FP8 reference cache

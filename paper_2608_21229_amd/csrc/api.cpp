@@ -519,6 +519,162 @@ rc_status plan_bwd(const rc_layout* L, BwdParams& b) {
   return RC_OK;
 }
 
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+rc_status check_float_ptr(const float* p, const char* name) { return check_lse(p, name); }
+
+// What both directions of the rotation check, and the parameters they share.
+rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* a, const void* b,
+                        const char* names, const void* positions, int32_t pos_float, int32_t pos_batch,
+                        const void* q_norm, const void* k_norm, float eps, RotaryParams& p) {
+  if (!R || R->n_axes < 1 || R->n_axes > RC_MAX_ROTARY_AXES || R->width < 0 || R->width > R->head_dim) {
+    set_error("rotary: the description is not one that rc_rotary_init has filled");
+    return RC_ERR_ARG;
+  }
+  if (R->head_dim != 64 && R->head_dim != 128) {
+    set_error("head_dim %d is not supported (64 or 128)", R->head_dim);
+    return RC_ERR_UNSUPPORTED;
+  }
+  if (B < 1 || H < 1 || B > 65535 || H > 65535 || N < 0 || N > (int64_t(1) << 31) / B - 1) {
+    set_error("B = %d, H = %d: each must be in [1, 65535]; N = %lld: B * N below 2^31", B, H, (long long)N);
+    return RC_ERR_ARG;
+  }
+  if (N > 0 && !a && !b) {
+    set_error("%s are both null", names);
+    return RC_ERR_ARG;
+  }
+  if ((q_norm || k_norm) && !(eps >= 0.f && isfinite(eps))) {
+    set_error("eps must be finite and >= 0 (got %g)", (double)eps);
+    return RC_ERR_ARG;
+  }
+  if (N > 0 && ((q_norm && !a) || (k_norm && !b))) {
+    set_error("a norm without its tensor");
+    return RC_ERR_ARG;
+  }
+  if (q_norm) RC_TRY(check_ptr(q_norm, "q_norm"));
+  if (k_norm) RC_TRY(check_ptr(k_norm, "k_norm"));
+  if (N > 0) {
+    if (!positions || (reinterpret_cast<uintptr_t>(positions) & 3u)) {
+      set_error("positions is null or not 4-byte aligned");
+      return RC_ERR_ARG;
+    }
+  }
+  memset(&p, 0, sizeof p);
+  p.pos = positions;
+  p.pos_float = pos_float != 0;
+  p.pos_sb = pos_batch ? N * R->n_axes : 0;
+  p.w[0] = static_cast<const uint16_t*>(q_norm);
+  p.w[1] = static_cast<const uint16_t*>(k_norm);
+  p.N = N;
+  p.B = B;
+  p.H = H;
+  p.axes = R->n_axes;
+  p.eps = eps;
+  p.half = R->interleaved ? 0 : R->width / 2;
+  for (int i = 0; i < R->head_dim / 2; ++i) {
+    const bool in = 2 * i < R->width;
+    if (in && (R->axis[i] >= R->n_axes || !isfinite(R->turns[i]))) {
+      set_error("rotary: the description is not one that rc_rotary_init has filled");
+      return RC_ERR_ARG;
+    }
+    p.axis[i] = in ? R->axis[i] : 0;
+    p.turns[i] = in ? R->turns[i] : 0.0;
+  }
+  return RC_OK;
+}
+
+// Row groups per wave: whole tokens (their sines are computed once) as long as
+// that leaves 16 waves per CU, fewer for few tokens.
+int32_t rotary_groups(const RotaryParams& p, int32_t D) {
+  const int rows = (p.x[0] ? p.H : 0) + (p.x[1] ? p.H : 0), rw = 512 / D;
+  const int64_t all = (rows + rw - 1) / rw;
+  const int64_t g = all * p.N * p.B / (16 * kCUs);
+  return int32_t(std::max<int64_t>(1, std::min<int64_t>({g, all, 12})));
+}
+
+int32_t rotary_blocks(int32_t B, int64_t N) {
+  return int32_t(std::max<int64_t>(1, std::min<int64_t>(kRotaryBlocks, (N * B + 3) / 4)));
+}
+
+rc_status check_rows(const void* ptr, int64_t ld, int32_t C, const char* name) {
+  RC_TRY(check_ptr(ptr, name));
+  if (ld < C || (ld & 7) || ld > (int64_t(1) << 22)) {
+    set_error("%s: row stride %lld must be >= C = %d, a multiple of 8, <= 2^22", name, (long long)ld, C);
+    return RC_ERR_ARG;
+  }
+  return RC_OK;
+}
+
+// Checks a gated norm's description and fills what both directions share.
+rc_status norm_params(const rc_norm* d, NormParams& p) {
+  memset(&p, 0, sizeof p);
+  if (!d) {
+    set_error("the description is null");
+    return RC_ERR_ARG;
+  }
+  if (d->B < 1 || d->B > 65535 || d->N < 0 || d->N > (int64_t(1) << 31) / d->B - 1 || d->C < 8 || d->C > kNormMaxC ||
+      d->C % 8 != 0) {
+    set_error("B = %d must be in [1, 65535], B * N below 2^31 (N = %lld), C = %d a multiple of 8 in [8, %d]", d->B,
+              (long long)d->N, d->C, kNormMaxC);
+    return RC_ERR_ARG;
+  }
+  if (d->n_groups < 1 || d->n_groups > 65535 || d->n_spans < 0 || d->n_spans > RC_MAX_SEGMENTS ||
+      (d->norm != RC_NORM_LAYER && d->norm != RC_NORM_RMS)) {
+    set_error("n_groups = %d, n_spans = %d, norm = %d: out of range", d->n_groups, d->n_spans, d->norm);
+    return RC_ERR_ARG;
+  }
+  if (!(d->eps >= 0.f && isfinite(d->eps)) || !isfinite(d->residual_scale)) {
+    set_error("eps must be finite and >= 0, residual_scale finite (got %g, %g)", (double)d->eps,
+              (double)d->residual_scale);
+    return RC_ERR_ARG;
+  }
+  if (d->mod_batch < 0 || d->mod_group < 0 || (d->mod_batch & 7) || (d->mod_group & 7)) {
+    set_error("mod strides %lld, %lld must be multiples of 8, >= 0", (long long)d->mod_batch, (long long)d->mod_group);
+    return RC_ERR_ARG;
+  }
+  int64_t n = 0;
+  for (int s = 0; s < d->n_spans; ++s) {
+    if (d->rows[s] < 0 || d->group[s] < 0 || d->group[s] >= d->n_groups) {
+      set_error("span %d: %d rows of group %d (of %d)", s, d->rows[s], d->group[s], d->n_groups);
+      return RC_ERR_ARG;
+    }
+    if (d->rows[s] == 0) continue;
+    p.span_row0[p.n_spans] = int32_t(std::min<int64_t>(n, INT32_MAX));
+    p.span_rows[p.n_spans] = d->rows[s];
+    p.span_group[p.n_spans++] = d->group[s];
+    n += d->rows[s];
+  }
+  if (n != d->N) {
+    set_error("the spans have %lld rows, the batch entries %lld", (long long)n, (long long)d->N);
+    return RC_ERR_ARG;
+  }
+  p.mod_sb = d->mod_batch;
+  p.mod_sg = d->mod_group;
+  p.N = d->N;
+  p.B = d->B;
+  p.C = d->C;
+  p.G = d->n_groups;
+  p.rms = d->norm == RC_NORM_RMS;
+  p.post = d->post != 0;
+  p.eps = d->eps;
+  p.rscale = d->residual_scale;
+  p.inv_c = 1.f / float(d->C);
+  // the backward's chunks: one work-group each, about one per CU, inside one span
+  const int64_t rows = d->N * d->B;
+  p.chunk_rows = int32_t(std::max<int64_t>(8, (rows + kCUs - 1) / kCUs));
+  for (int s = 0; s < p.n_spans; ++s) {
+    p.span_chunk0[s] = p.chunks;
+    p.chunks += (p.span_rows[s] + p.chunk_rows - 1) / p.chunk_rows;
+  }
+  return RC_OK;
+}
+
+rc_status check_vec(const void* p, const char* name) { return p ? check_ptr(p, name) : RC_OK; }
+
+NormRows rows_of(const void* p, int64_t ld) { return NormRows{static_cast<uint16_t*>(const_cast<void*>(p)), ld}; }
+
+size_t norm_partial_bytes(const NormParams& p) { return size_t(p.B) * p.chunks * 3 * p.C * sizeof(float); }
+
 // Per-row statistics of the gradient: two floats per (batch, head, row), each
 // in a 16-byte aligned array.
 size_t bwd_row_bytes(int64_t rows) { return (size_t(rows) * sizeof(float) + 15) & ~size_t(15); }
@@ -854,6 +1010,276 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
   RC_TRY(hip_status(launch_attention_bwd(p, D, stream), "attention gradient launch"));
+  return RC_OK;
+}
+
+rc_status rc_rotary_init(rc_rotary* R, int32_t head_dim, int32_t n_axes, const int32_t* axes, double theta,
+                         int32_t interleaved, int32_t continuous) {
+  if (!R || !axes || n_axes < 1 || n_axes > RC_MAX_ROTARY_AXES) {
+    set_error("rotary: null argument, or n_axes = %d not in [1, %d]", n_axes, RC_MAX_ROTARY_AXES);
+    return RC_ERR_ARG;
+  }
+  if (head_dim != 64 && head_dim != 128) {
+    set_error("head_dim %d is not supported (64 or 128)", head_dim);
+    return RC_ERR_UNSUPPORTED;
+  }
+  if (!(theta > 0.0) || !isfinite(theta)) {
+    set_error("theta must be finite and > 0 (got %g)", theta);
+    return RC_ERR_ARG;
+  }
+  int64_t width = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (axes[a] < 0 || axes[a] % 2 != 0 || (width += axes[a]) > head_dim) {
+      set_error("axis %d: width %d must be even, and the widths add up to at most %d", a, axes[a], head_dim);
+      return RC_ERR_ARG;
+    }
+  }
+  if (!interleaved && width % 16 != 0) {
+    set_error("pairs of halves need a rotated width that is a multiple of 16 (got %lld)", (long long)width);
+    return RC_ERR_UNSUPPORTED;
+  }
+  memset(R, 0, sizeof *R);
+  R->head_dim = head_dim;
+  R->n_axes = n_axes;
+  R->width = int32_t(width);
+  R->interleaved = interleaved != 0;
+  int p = 0;
+  for (int a = 0; a < n_axes; ++a)
+    for (int i = 0; i < axes[a] / 2; ++i, ++p) {
+      const double e = continuous ? 2.0 * p / double(width) : 2.0 * i / double(axes[a]);
+      R->axis[p] = uint8_t(a);
+      R->turns[p] = pow(theta, -e) / kTwoPi;
+    }
+  return RC_OK;
+}
+
+rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* q, const void* k,
+                       int64_t tok_stride, const void* positions, int32_t pos_float, int32_t pos_batch,
+                       const void* q_norm, const void* k_norm, float eps, void* q_out, void* k_out,
+                       int64_t out_stride, void* stream) {
+  RotaryParams p;
+  RC_TRY(rotary_params(R, B, N, H, q, k, "q and k", positions, pos_float, pos_batch, q_norm, k_norm, eps, p));
+  const int32_t D = R->head_dim;
+  RC_TRY(check_stride(tok_stride, H, D));
+  RC_TRY(check_stride(out_stride, H, D));
+  if (N == 0) return RC_OK;
+  const void* in[2] = {q, k};
+  void* out[2] = {q_out, k_out};
+  for (int i = 0; i < 2; ++i) {
+    if (!in[i]) continue;
+    RC_TRY(check_ptr(in[i], i ? "k" : "q"));
+    RC_TRY(check_ptr(out[i], i ? "k_out" : "q_out"));
+    if (in[i] == out[i] && tok_stride != out_stride) {
+      set_error("%s in place needs the input's token stride", i ? "k" : "q");
+      return RC_ERR_ARG;
+    }
+    p.x[i] = static_cast<const uint16_t*>(in[i]);
+    p.y[i] = static_cast<uint16_t*>(out[i]);
+  }
+  p.x_st = tok_stride;
+  p.y_st = out_stride;
+  p.sign = 1.f;
+  p.groups = rotary_groups(p, D);
+  RC_TRY(check_blocks(B * N * ((2 * int64_t(H) * D + 511) / 512), "rotation"));
+  RC_TRY(check_launcher(launch_rotary, "rotation"));
+  RC_TRY(hip_status(launch_rotary(p, D, stream), "rotation launch"));
+  return RC_OK;
+}
+
+size_t rc_rotary_backward_workspace_bytes(const rc_rotary* R, int32_t B, int64_t N) {
+  if (!R || (R->head_dim != 64 && R->head_dim != 128) || B < 1 || N < 0) return 0;
+  return size_t(rotary_blocks(B, N)) * 2 * R->head_dim * sizeof(float);
+}
+
+rc_status rc_qk_rotary_backward(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* dq, const void* dk,
+                                int64_t grad_stride, const void* positions, int32_t pos_float, int32_t pos_batch,
+                                const void* q, const void* k, int64_t tok_stride, const void* q_norm,
+                                const void* k_norm, float eps, void* dq_in, void* dk_in, int64_t out_stride,
+                                float* dq_norm, float* dk_norm, void* workspace, size_t ws_bytes, void* stream) {
+  RotaryParams p;
+  RC_TRY(rotary_params(R, B, N, H, dq, dk, "dq and dk", positions, pos_float, pos_batch, q_norm, k_norm, eps, p));
+  const int32_t D = R->head_dim;
+  const bool norm = q_norm || k_norm;
+  RC_TRY(check_stride(grad_stride, H, D));
+  RC_TRY(check_stride(out_stride, H, D));
+  if (norm) RC_TRY(check_stride(tok_stride, H, D));
+  if ((dq_norm && !q_norm) || (dk_norm && !k_norm)) {
+    set_error("the gradient of a norm that is not there");
+    return RC_ERR_ARG;
+  }
+  RC_TRY(check_float_ptr(dq_norm, "dq_norm"));
+  RC_TRY(check_float_ptr(dk_norm, "dk_norm"));
+  const void* g[2] = {dq, dk};
+  const void* n[2] = {q, k};
+  void* out[2] = {dq_in, dk_in};
+  for (int i = 0; i < 2 && N > 0; ++i) {
+    if (!g[i]) continue;
+    RC_TRY(check_ptr(g[i], i ? "dk" : "dq"));
+    RC_TRY(check_ptr(out[i], i ? "dk_in" : "dq_in"));
+    if (p.w[i]) RC_TRY(check_ptr(n[i], i ? "k" : "q"));
+    if (g[i] == out[i] && grad_stride != out_stride) {
+      set_error("%s in place needs the input's token stride", i ? "dk" : "dq");
+      return RC_ERR_ARG;
+    }
+    p.x[i] = static_cast<const uint16_t*>(g[i]);
+    p.n[i] = static_cast<const uint16_t*>(n[i]);
+    p.y[i] = static_cast<uint16_t*>(out[i]);
+  }
+  p.x_st = grad_stride;
+  p.n_st = tok_stride;
+  p.y_st = out_stride;
+  p.sign = -1.f;
+  RC_TRY(check_blocks(B * N * ((2 * int64_t(H) * D + 511) / 512), "rotation gradient"));
+  if (!norm) {
+    if (N == 0) return RC_OK;
+    p.groups = rotary_groups(p, D);
+    RC_TRY(check_launcher(launch_rotary, "rotation gradient"));
+    RC_TRY(hip_status(launch_rotary(p, D, stream), "rotation gradient launch"));
+    return RC_OK;
+  }
+  const size_t need = rc_rotary_backward_workspace_bytes(R, B, N);
+  if (!workspace || !aligned16(workspace) || ws_bytes < need) {
+    set_error("the rotation's gradient with a norm needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+              workspace ? ws_bytes : size_t(0));
+    return RC_ERR_WORKSPACE;
+  }
+  p.partial = static_cast<float*>(workspace);
+  p.dw[0] = dq_norm;
+  p.dw[1] = dk_norm;
+  p.blocks = rotary_blocks(B, N);
+  RC_TRY(check_launcher(launch_rotary_norm_backward, "rotation gradient"));
+  RC_TRY(hip_status(launch_rotary_norm_backward(p, D, stream), "rotation gradient launch"));
+  return RC_OK;
+}
+
+rc_status rc_gated_norm(const rc_norm* d, const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,
+                        const void* scale, const void* shift, const void* weight, const void* post_weight,
+                        void* h_out, int64_t ldho, void* y, int64_t ldy, void* stream) {
+  NormParams p;
+  RC_TRY(norm_params(d, p));
+  if (p.N > 0 &&
+      ((x == nullptr) != (h_out == nullptr) || (!x && (gate || post_weight || p.post)) || (!x && !y))) {
+    set_error("gated norm: x and h_out go together, gate and the norm after the block with x; y without x");
+    return RC_ERR_ARG;
+  }
+  if (post_weight && !p.post) {
+    set_error("post_weight without the norm after the block");
+    return RC_ERR_ARG;
+  }
+  if (p.N > 0 && !y && (scale || shift || weight)) {
+    set_error("scale, shift and weight belong to y");
+    return RC_ERR_ARG;
+  }
+  if (p.N == 0) return RC_OK;
+  RC_TRY(check_rows(h, ldh, p.C, "h"));
+  if (x) {
+    RC_TRY(check_rows(x, ldx, p.C, "x"));
+    RC_TRY(check_rows(h_out, ldho, p.C, "h_out"));
+    if (h_out == h && ldho != ldh) {
+      set_error("h_out in place needs h's row stride");
+      return RC_ERR_ARG;
+    }
+  }
+  if (y) RC_TRY(check_rows(y, ldy, p.C, "y"));
+  RC_TRY(check_vec(gate, "gate"));
+  RC_TRY(check_vec(scale, "scale"));
+  RC_TRY(check_vec(shift, "shift"));
+  RC_TRY(check_vec(weight, "weight"));
+  RC_TRY(check_vec(post_weight, "post_weight"));
+  p.h = rows_of(h, ldh);
+  p.x = rows_of(x, ldx);
+  p.h_out = rows_of(h_out, ldho);
+  p.y = rows_of(y, ldy);
+  p.gate = static_cast<const uint16_t*>(gate);
+  p.scale = static_cast<const uint16_t*>(scale);
+  p.shift = static_cast<const uint16_t*>(shift);
+  p.weight = static_cast<const uint16_t*>(weight);
+  p.post_weight = static_cast<const uint16_t*>(post_weight);
+  RC_TRY(check_launcher(launch_norm, "gated norm"));
+  RC_TRY(hip_status(launch_norm(p, stream), "gated norm launch"));
+  return RC_OK;
+}
+
+size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d) {
+  NormParams p;
+  return norm_params(d, p) == RC_OK ? norm_partial_bytes(p) : 0;
+}
+
+rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy, const void* dh, int64_t lddh,
+                                 const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,
+                                 const void* scale, const void* weight, const void* post_weight, void* dh_in,
+                                 int64_t lddhi, void* dx, int64_t lddx, float* dgate, float* dscale, float* dshift,
+                                 float* dweight, float* dpost_weight, void* workspace, size_t ws_bytes,
+                                 void* stream) {
+  NormParams p;
+  RC_TRY(norm_params(d, p));
+  if (p.N > 0 &&
+      ((x == nullptr) != (dx == nullptr) || (!x && (gate || post_weight || p.post || dgate || dpost_weight)))) {
+    set_error("gated norm: x and dx go together, gate and the norm after the block with x");
+    return RC_ERR_ARG;
+  }
+  if (post_weight && !p.post) {
+    set_error("post_weight without the norm after the block");
+    return RC_ERR_ARG;
+  }
+  if (p.N > 0 && ((!dy && (scale || weight || dscale || dshift || dweight)) || (!dy && !dh))) {
+    set_error("without dy there is only dh, no scale, shift or weight");
+    return RC_ERR_ARG;
+  }
+  if ((dweight && !weight) || (dpost_weight && !post_weight) || (dgate && !gate)) {
+    set_error("the gradient of a vector that is not there");
+    return RC_ERR_ARG;
+  }
+  if (p.N > 0) {
+    if (dy) {
+      RC_TRY(check_rows(dy, lddy, p.C, "dy"));
+      RC_TRY(check_rows(h, ldh, p.C, "h"));
+    }
+    if (dh) RC_TRY(check_rows(dh, lddh, p.C, "dh"));
+    RC_TRY(check_rows(dh_in, lddhi, p.C, "dh_in"));
+    if (x) {
+      RC_TRY(check_rows(x, ldx, p.C, "x"));
+      RC_TRY(check_rows(dx, lddx, p.C, "dx"));
+    }
+    if ((dh_in == dh && lddhi != lddh) || (dh_in == dy && lddhi != lddy) || (x && dx == x && lddx != ldx)) {
+      set_error("a gradient in place needs its input's row stride");
+      return RC_ERR_ARG;
+    }
+  }
+  RC_TRY(check_vec(gate, "gate"));
+  RC_TRY(check_vec(scale, "scale"));
+  RC_TRY(check_vec(weight, "weight"));
+  RC_TRY(check_vec(post_weight, "post_weight"));
+  const struct {
+    const float* p;
+    const char* name;
+  } outs[] = {{dgate, "dgate"}, {dscale, "dscale"}, {dshift, "dshift"}, {dweight, "dweight"},
+              {dpost_weight, "dpost_weight"}};
+  for (const auto& o : outs) RC_TRY(check_float_ptr(o.p, o.name));
+  const size_t need = norm_partial_bytes(p);
+  if (need > 0 && (!workspace || !aligned16(workspace) || ws_bytes < need)) {
+    set_error("the gated norm's gradient needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+              workspace ? ws_bytes : size_t(0));
+    return RC_ERR_WORKSPACE;
+  }
+  p.dy = rows_of(dy, lddy);
+  p.dh = rows_of(dh, lddh);
+  p.h = rows_of(h, ldh);
+  p.x = rows_of(x, ldx);
+  p.dh_in = rows_of(dh_in, lddhi);
+  p.dx = rows_of(dx, lddx);
+  p.gate = static_cast<const uint16_t*>(gate);
+  p.scale = static_cast<const uint16_t*>(scale);
+  p.weight = static_cast<const uint16_t*>(weight);
+  p.post_weight = static_cast<const uint16_t*>(post_weight);
+  p.dgate = dgate;
+  p.dscale = dscale;
+  p.dshift = dshift;
+  p.dweight = dweight;
+  p.dpost_weight = dpost_weight;
+  p.partial = static_cast<float*>(workspace);
+  RC_TRY(check_launcher(launch_norm_backward, "gated norm gradient"));
+  RC_TRY(hip_status(launch_norm_backward(p, stream), "gated norm gradient launch"));
   return RC_OK;
 }
 

@@ -1,0 +1,434 @@
+// Gated norm between two blocks of a layer: the residual with the block's
+// gated output, then the norm and modulation that the next block reads.
+//   u  = x, or w_p x rsqrt(mean x^2 + eps)
+//   h' = h + a gate u
+//   y  = n(h') w (1 + scale) + shift,  n the layer norm without affine, or the RMS norm
+// gate, scale and shift belong to a row's group (one vector per batch entry and
+// group).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "rc_layer.h"
+
+namespace rc {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ bf16x8 load8(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  bf16x8 o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = (__bf16)v[e];
+  *reinterpret_cast<bf16x8*>(p) = o;
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+  return x;
+}
+
+// Sums over the T threads of a row.  Each array has two halves that take turns,
+// so that one barrier per sum is enough: a half is written again only after
+// the next sum's barrier, which every reader of it has reached.
+template <int K>
+struct RowSums {
+  float at[2][16][K];
+};
+template <int T, int K>
+__device__ __forceinline__ void row_sums(float (&x)[K], RowSums<K>& lds, int row, int& half) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+  if constexpr (T > 64) {
+    constexpr int W = T / 64;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) lds.at[half][wave][k] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += lds.at[half][row * W + w][k];
+      x[k] = s;
+    }
+    half ^= 1;
+  }
+}
+
+__device__ __forceinline__ int group_of(const NormParams& p, int n) {
+  int s = 0;
+  while (s + 1 < p.n_spans && p.span_row0[s + 1] <= n) ++s;
+  return p.span_group[s];
+}
+
+// T threads per row, GP granules of 8 channels per thread.
+template <int T, int GP>
+__global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
+  __shared__ RowSums<1> lds;
+  constexpr int RB = 256 / T;
+  const int t = threadIdx.x % T, rb = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+  const uint32_t N = uint32_t(p.N), r_ = blockIdx.x * RB + rb;
+  const bool in = r_ < N * p.B;
+  const uint32_t r32 = in ? r_ : 0, b = r32 / N;
+  const int64_t r = r32;
+  const int64_t mod = b * p.mod_sb + int64_t(group_of(p, int(r32 - b * N))) * p.mod_sg;
+  const int ng = p.C / 8;
+  int half = 0;
+  float h[GP][8];
+#pragma unroll
+  for (int i = 0; i < GP; ++i) {
+    const int g = t + i * T;
+    const bool has = g < ng;
+    const bf16x8 a = has ? load8(p.h.p + r * p.h.ld + g * 8) : bf16x8{};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[i][e] = float(a[e]);
+  }
+  if (p.x.p) {
+    float x[GP][8], k[1] = {1.f};
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int g = t + i * T;
+      const bf16x8 a = g < ng ? load8(p.x.p + r * p.x.ld + g * 8) : bf16x8{};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = float(a[e]);
+    }
+    if (p.post) {
+      k[0] = 0.f;
+#pragma unroll
+      for (int i = 0; i < GP; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[0] += x[i][e] * x[i][e];
+      row_sums<T, 1>(k, lds, rb, half);
+      k[0] = rsqrtf(k[0] * p.inv_c + p.eps);
+    }
+    const float f = k[0] * p.rscale;
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int g = t + i * T;
+      if (g >= ng) continue;
+      if (p.post_weight) {
+        const bf16x8 w = load8(p.post_weight + g * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] *= float(w[e]);
+      }
+      if (p.gate) {
+        const bf16x8 w = load8(p.gate + mod + g * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] *= float(w[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] += f * x[i][e];
+      if (in) store8(p.h_out.p + r * p.h_out.ld + g * 8, h[i]);
+    }
+  }
+  if (!p.y.p) return;
+  if (!p.rms) {
+    float m[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < GP; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m[0] += h[i][e];
+    row_sums<T, 1>(m, lds, rb, half);
+    const float mean = m[0] * p.inv_c;
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      if (t + i * T >= ng) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] -= mean;
+    }
+  }
+  float v[1] = {0.f};
+#pragma unroll
+  for (int i = 0; i < GP; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[0] += h[i][e] * h[i][e];
+  row_sums<T, 1>(v, lds, rb, half);
+  const float rs = rsqrtf(v[0] * p.inv_c + p.eps);
+#pragma unroll
+  for (int i = 0; i < GP; ++i) {
+    const int g = t + i * T;
+    if (g >= ng) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[i][e] *= rs;
+    if (p.weight) {
+      const bf16x8 w = load8(p.weight + g * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] *= float(w[e]);
+    }
+    if (p.scale) {
+      const bf16x8 w = load8(p.scale + mod + g * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] += h[i][e] * float(w[e]);
+    }
+    if (p.shift) {
+      const bf16x8 w = load8(p.shift + mod + g * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] += float(w[e]);
+    }
+    if (in) store8(p.y.p + r * p.y.ld + g * 8, h[i]);
+  }
+}
+
+// Backward: a work-group of NT threads takes one chunk of rows of one batch
+// entry and span, NT / T rows at a time, and leaves the chunk's sums over its
+// rows of dy, dy n and dh' x^ (the gradients of shift, scale and gate up to
+// factors of the column).
+template <int T, int GP, int NT>
+__global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
+  __shared__ RowSums<1> lds1;
+  __shared__ RowSums<3> lds3;
+  extern __shared__ float acc_lds[];
+  constexpr int RB = NT / T;
+  const int t = threadIdx.x % T, rb = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+  const int64_t b = blockIdx.x / p.chunks;
+  const int chunk = blockIdx.x % p.chunks;
+  int sp = 0;
+  while (sp + 1 < p.n_spans && p.span_chunk0[sp + 1] <= chunk) ++sp;
+  const int first = (chunk - p.span_chunk0[sp]) * p.chunk_rows;
+  const int count = min(p.chunk_rows, p.span_rows[sp] - first);
+  const int64_t row0 = b * p.N + p.span_row0[sp] + first;
+  const int64_t mod = b * p.mod_sb + int64_t(p.span_group[sp]) * p.mod_sg;
+  const int ng = p.C / 8;
+  int half1 = 0, half3 = 0;
+  float a_shift[GP][8], a_scale[GP][8], a_gate[GP][8];
+#pragma unroll
+  for (int i = 0; i < GP; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a_shift[i][e] = a_scale[i][e] = a_gate[i][e] = 0.f;
+  for (int i0 = 0; i0 < count; i0 += RB) {
+    const bool in = i0 + rb < count;
+    const int64_t r = row0 + (in ? i0 + rb : 0);
+    float n[GP][8], d[GP][8], dh[GP][8];
+    float m[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int g = t + i * T;
+      const bool has = g < ng && in;
+      const bf16x8 a = p.dh.p && has ? load8(p.dh.p + r * p.dh.ld + g * 8) : bf16x8{};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dh[i][e] = float(a[e]);
+    }
+    if (p.dy.p) {
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const int g = t + i * T;
+        const bool has = g < ng && in;
+        const bf16x8 a = has ? load8(p.h.p + r * p.h.ld + g * 8) : bf16x8{};
+        const bf16x8 c = has ? load8(p.dy.p + r * p.dy.ld + g * 8) : bf16x8{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          n[i][e] = float(a[e]);
+          d[i][e] = float(c[e]);
+          m[0] += n[i][e];
+        }
+      }
+      if (!p.rms) {
+        row_sums<T, 1>(m, lds1, rb, half1);
+        const float mean = m[0] * p.inv_c;
+#pragma unroll
+        for (int i = 0; i < GP; ++i) {
+          if (t + i * T >= ng || !in) continue;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) n[i][e] -= mean;
+        }
+      }
+      // over the row: n^2, dn, dn n (dn = dy (1 + scale) w)
+      float k[3] = {0.f, 0.f, 0.f};
+      float dn[GP][8];
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const int g = t + i * T;
+        bf16x8 ws{}, ww{};
+        if (p.scale && g < ng) ws = load8(p.scale + mod + g * 8);
+        if (p.weight && g < ng) ww = load8(p.weight + g * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float x = d[i][e] + d[i][e] * float(ws[e]);
+          if (p.weight) x *= float(ww[e]);
+          dn[i][e] = x;
+          k[0] += n[i][e] * n[i][e];
+          k[1] += x;
+          k[2] += x * n[i][e];
+        }
+      }
+      row_sums<T, 3>(k, lds3, rb, half3);
+      const float rs = rsqrtf(k[0] * p.inv_c + p.eps);
+      const float mean = p.rms ? 0.f : k[1] * p.inv_c, dot = k[2] * p.inv_c * rs * rs;
+#pragma unroll
+      for (int i = 0; i < GP; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          a_shift[i][e] += d[i][e];
+          a_scale[i][e] += d[i][e] * n[i][e] * rs;
+          dh[i][e] += rs * (dn[i][e] - mean - n[i][e] * dot);
+        }
+    }
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const int g = t + i * T;
+        if (g < ng) store8(p.dh_in.p + r * p.dh_in.ld + g * 8, dh[i]);
+      }
+    }
+    if (!p.x.p) continue;
+    float x[GP][8], k[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int g = t + i * T;
+      const bool has = g < ng && in;
+      const bf16x8 a = has ? load8(p.x.p + r * p.x.ld + g * 8) : bf16x8{};
+      bf16x8 wg{}, ww{};
+      if (p.gate && g < ng) wg = load8(p.gate + mod + g * 8);
+      if (p.post_weight && g < ng) ww = load8(p.post_weight + g * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[i][e] = float(a[e]);
+        float du = p.rscale * dh[i][e];
+        d[i][e] = has ? du : 0.f;
+        if (p.gate) du *= float(wg[e]);
+        if (p.post_weight) du *= float(ww[e]);
+        dh[i][e] = du;
+        k[0] += x[i][e] * x[i][e];
+        k[1] += du * x[i][e];
+      }
+    }
+    float rx = 1.f, dot = 0.f;
+    if (p.post) {
+      row_sums<T, 3>(k, lds3, rb, half3);
+      rx = rsqrtf(k[0] * p.inv_c + p.eps);
+      dot = k[1] * p.inv_c * rx * rx;
+    }
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int g = t + i * T;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        a_gate[i][e] += d[i][e] * x[i][e] * rx;
+        dh[i][e] = rx * (dh[i][e] - x[i][e] * dot);
+      }
+      if (in && g < ng) store8(p.dx.p + r * p.dx.ld + g * 8, dh[i]);
+    }
+  }
+  // the row groups' sums, in order, through LDS
+  float* out = p.partial + int64_t(blockIdx.x) * 3 * p.C;
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    auto& a = q == 0 ? a_shift : q == 1 ? a_scale : a_gate;
+    if constexpr (RB > 1) {
+      __syncthreads();
+      for (int w = 0; w < RB; ++w) {
+        if (rb == w) {
+#pragma unroll
+          for (int i = 0; i < GP; ++i) {
+            const int g = t + i * T;
+            if (g < ng)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc_lds[g * 8 + e] = w == 0 ? a[i][e] : acc_lds[g * 8 + e] + a[i][e];
+          }
+        }
+        __syncthreads();
+      }
+      for (int c = threadIdx.x; c < p.C; c += NT) out[q * p.C + c] = acc_lds[c];
+    } else {
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const int g = t + i * T;
+        if (g < ng)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) out[q * p.C + g * 8 + e] = a[i][e];
+      }
+    }
+  }
+}
+
+// The gradients shared between rows from the chunks' sums: 64 columns per
+// work-group, each of its 16 waves a share of the chunks.
+__global__ __launch_bounds__(1024) void norm_shared_kernel(const NormParams p) {
+  __shared__ float part[16][3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const bool in = c < p.C;
+  float dw = 0.f, dwp = 0.f;
+  const auto bf = [&](const uint16_t* v, int64_t at) { return __uint_as_float(uint32_t(v[at]) << 16); };
+  for (int b = 0; b < p.B; ++b)
+    for (int g = 0; g < p.G; ++g) {
+      float a[3] = {0.f, 0.f, 0.f};
+      for (int s = 0; s < p.n_spans; ++s) {
+        if (p.span_group[s] != g) continue;
+        const int end = s + 1 < p.n_spans ? p.span_chunk0[s + 1] : p.chunks;
+        for (int k = p.span_chunk0[s] + wave; k < end && in; k += 16) {
+          const float* q = p.partial + (int64_t(b) * p.chunks + k) * 3 * p.C + c;
+          a[0] += q[0];
+          a[1] += q[p.C];
+          a[2] += q[2 * int64_t(p.C)];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < 3; ++q) part[wave][q][lane] = a[q];
+      __syncthreads();
+      if (wave != 0 || !in) continue;
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        a[q] = 0.f;
+        for (int w = 0; w < 16; ++w) a[q] += part[w][q][lane];
+      }
+      const int64_t mod = b * p.mod_sb + int64_t(g) * p.mod_sg + c, at = (int64_t(b) * p.G + g) * p.C + c;
+      if (p.dshift) p.dshift[at] = a[0];
+      if (p.dscale) p.dscale[at] = a[1] * (p.weight ? bf(p.weight, c) : 1.f);
+      if (p.dgate) p.dgate[at] = a[2] * (p.post_weight ? bf(p.post_weight, c) : 1.f);
+      dw += a[1] * (p.scale ? 1.f + bf(p.scale, mod) : 1.f);
+      dwp += a[2] * (p.gate ? bf(p.gate, mod) : 1.f);
+    }
+  if (wave != 0 || !in) return;
+  if (p.dweight) p.dweight[c] = dw;
+  if (p.dpost_weight) p.dpost_weight[c] = dwp;
+}
+
+template <int T, int GP>
+void launch_fwd(const NormParams& p, hipStream_t s) {
+  const int64_t rows = p.N * p.B;
+  hipLaunchKernelGGL((norm_kernel<T, GP>), dim3((rows + 256 / T - 1) / (256 / T)), dim3(256), 0, s, p);
+}
+template <int T, int GP>
+void launch_bwd(const NormParams& p, hipStream_t s) {
+  constexpr int NT = 512;
+  if (p.chunks > 0)
+    hipLaunchKernelGGL((norm_backward_kernel<T, GP, NT>), dim3(int64_t(p.B) * p.chunks), dim3(NT),
+                       NT > T ? p.C * sizeof(float) : 0, s, p);
+  hipLaunchKernelGGL(norm_shared_kernel, dim3((p.C + 63) / 64), dim3(1024), 0, s, p);
+}
+
+}  // namespace
+
+int launch_norm(const NormParams& p, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int ng = p.C / 8;
+  if (ng <= 64) launch_fwd<64, 1>(p, s);
+  else if (ng <= 128) launch_fwd<64, 2>(p, s);
+  else if (ng <= 192) launch_fwd<64, 3>(p, s);
+  else if (ng <= 256) launch_fwd<64, 4>(p, s);
+  else if (ng <= 320) launch_fwd<64, 5>(p, s);
+  else if (ng <= 384) launch_fwd<64, 6>(p, s);
+  else if (ng <= 512) launch_fwd<64, 8>(p, s);
+  else if (ng <= 1024) launch_fwd<256, 4>(p, s);
+  else launch_fwd<256, 8>(p, s);
+  return int(hipGetLastError());
+}
+
+int launch_norm_backward(const NormParams& p, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int ng = p.C / 8;
+  if (ng <= 64) launch_bwd<64, 1>(p, s);
+  else if (ng <= 128) launch_bwd<64, 2>(p, s);
+  else if (ng <= 256) launch_bwd<128, 2>(p, s);
+  else if (ng <= 384) launch_bwd<128, 3>(p, s);
+  else if (ng <= 512) launch_bwd<256, 2>(p, s);
+  else if (ng <= 1024) launch_bwd<512, 2>(p, s);
+  else launch_bwd<512, 4>(p, s);
+  return int(hipGetLastError());
+}
+
+}  // namespace rc

@@ -49,4 +49,51 @@ struct BwdParams {
 };
 int launch_attention_bwd(const BwdParams& p, int D, void* stream) RC_WEAK;
 
+// ---------------------------------------------------------------- rotation
+struct RotaryParams {
+  const uint16_t* x[2];   // queries, keys (null: none); backward: the gradients of the outputs
+  const uint16_t* n[2];   // backward with a norm: its inputs
+  uint16_t* y[2];
+  const uint16_t* w[2];   // norm weights [D], null: no norm
+  float* dw[2];           // backward: their gradients
+  float* partial;         // backward: [blocks, 2, D] sums of dw
+  const void* pos;        // [N, axes] or [B, N, axes], int32 or fp32
+  int64_t x_st, n_st, y_st, pos_sb;
+  int64_t N;
+  int32_t B, H, axes, pos_float;
+  int32_t groups;         // row groups (64 lanes of 16 bytes each) per wave
+  int32_t blocks;         // backward with a norm: work-groups of the first pass
+  float eps, sign;        // sign: -1 turns back
+  int32_t half;           // > 0: channel p pairs with p + half; 0: 2p with 2p + 1
+  uint8_t axis[64];
+  double turns[64];       // per pair, revolutions per unit of position; 0 past the rotated width
+};
+int launch_rotary(const RotaryParams& p, int D, void* stream) RC_WEAK;
+int launch_rotary_norm_backward(const RotaryParams& p, int D, void* stream) RC_WEAK;
+constexpr int kRotaryBlocks = 1024;  // work-groups of the backward with a norm, at most
+
+// ---------------------------------------------------------------- gated norm
+struct NormRows {  // [B * N, C] rows
+  uint16_t* p;
+  int64_t ld;
+};
+struct NormParams {
+  NormRows h, x, h_out, y;            // forward
+  NormRows dy, dh, dh_in, dx;         // backward (h: the rows after the residual)
+  const uint16_t *gate, *scale, *shift, *weight, *post_weight;
+  float *dgate, *dscale, *dshift, *dweight, *dpost_weight;
+  float* partial;                     // [B, chunks, 3, C]
+  int64_t mod_sb, mod_sg;             // element strides of gate, scale and shift
+  int64_t N;
+  int32_t B, C, G, rms, post;
+  float eps, rscale, inv_c;
+  int32_t n_spans;
+  int32_t chunk_rows, chunks;         // backward: rows of a chunk (inside one span), chunks per batch entry
+  int32_t span_row0[RC_MAX_SEGMENTS], span_rows[RC_MAX_SEGMENTS], span_group[RC_MAX_SEGMENTS];
+  int32_t span_chunk0[RC_MAX_SEGMENTS];
+};
+constexpr int kNormMaxC = 16384;
+int launch_norm(const NormParams& p, void* stream) RC_WEAK;
+int launch_norm_backward(const NormParams& p, void* stream) RC_WEAK;
+
 }  // namespace rc
