@@ -464,13 +464,18 @@ def full_attention_backward(layout: Layout, q, k, v, o, lse, do, dq=None, dk=Non
     B, N, H, D = q.shape
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     ts = _tok_stride(q, k, v)
-    if lse is None:
-        raise ValueError("full_attention_backward: pass the forward's lse (want_lse=True)")
-    grads = [g if g is not None else _empty((B, N, H, D), torch.bfloat16, dev, stream) for g in (dq, dk, dv)]
-    for name, t in (("dq", grads[0]), ("dk", grads[1]), ("dv", grads[2])):
-        if t.dtype is not torch.bfloat16 or t.shape != q.shape:
-            raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(q.shape)}, got {str(t.dtype)} {tuple(t.shape)}")
-    gs = _tok_stride(*grads)
+    if o is None or lse is None or do is None:
+        raise ValueError("full_attention_backward: pass the forward's o and lse (want_lse=True) and do")
+    grads, gs = [dq, dk, dv], H * D
+    if dq is None and dk is None and dv is None:
+        grads = [_empty(q.shape, torch.bfloat16, dev, stream) for _ in grads]
+    else:
+        grads = [g if g is not None else _empty(q.shape, torch.bfloat16, dev, stream) for g in grads]
+        for name, t in zip(("dq", "dk", "dv"), grads):
+            if t.dtype is not torch.bfloat16 or t.shape != q.shape:
+                raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(q.shape)}, got {str(t.dtype)} "
+                                 f"{tuple(t.shape)}")
+        gs = _tok_stride(*grads)
     _expect(o, (B, N, H, D), "torch.bfloat16", "o")
     _expect(do, (B, N, H, D), "torch.bfloat16", "do")
     _expect(lse, (B, H, N), "torch.float32", "lse")
@@ -550,15 +555,33 @@ def _given(*ts):
     return [t for t in ts if t is not None]
 
 
+def _pair(names, q, k, D):
+    """The tensors given of a pair of queries and keys, checked: bf16
+    [B, N, H, D] on one GPU.  The first test covers the usual call."""
+    if q is not None and k is not None:
+        bf16 = _torch().bfloat16
+        if (q.dtype is bf16 and k.dtype is bf16 and q.is_cuda and q.device == k.device and q.shape == k.shape
+                and q.dim() == 4 and q.shape[3] == D):
+            return [q, k]
+    given = _given(q, k)
+    if not given:
+        raise ValueError(f"pass {names[0]}, {names[1]} or both")
+    for name, t in zip(names, (q, k)):
+        if t is not None:
+            _heads(name, t, given[0], D)
+    return given
+
+
 def _positions(rotary: Rotary, t, positions):
     """(is fp32, has a batch axis) of the positions of t's tokens."""
     torch = _torch()
-    B, N, A = t.shape[0], t.shape[1], len(rotary.axes)
-    if positions.dtype not in (torch.int32, torch.float32) or not positions.is_contiguous():
+    floats, shape, batch = positions.dtype is torch.float32, positions.shape, positions.dim() == 3
+    if not (floats or positions.dtype is torch.int32) or not positions.is_contiguous():
         raise ValueError(f"positions must be contiguous int32 or float32, got {str(positions.dtype)}")
-    if tuple(positions.shape) not in ((N, A), (B, N, A)):
-        raise ValueError(f"positions must be {(N, A)} or {(B, N, A)}, got {tuple(positions.shape)}")
-    return int(positions.dtype is torch.float32), int(positions.dim() == 3)
+    B, N, A = t.shape[0], t.shape[1], len(rotary.axes)
+    if shape != ((B, N, A) if batch else (N, A)):
+        raise ValueError(f"positions must be {(N, A)} or {(B, N, A)}, got {tuple(shape)}")
+    return int(floats), int(batch)
 
 
 def _norm_weight(name, w, D):
@@ -568,7 +591,11 @@ def _norm_weight(name, w, D):
 
 def _outputs(outs, ins, names, dev, stream):
     """An output per input (None where there is none), and their token stride."""
-    outs = [None if i is None else _empty(tuple(i.shape), i.dtype, dev, stream) if o is None else o
+    if outs[0] is None and outs[1] is None:
+        like = ins[0] if ins[0] is not None else ins[1]
+        shape = like.shape
+        return [None if i is None else _empty(shape, like.dtype, dev, stream) for i in ins], shape[2] * shape[3]
+    outs = [None if i is None else _empty(i.shape, i.dtype, dev, stream) if o is None else o
             for o, i in zip(outs, ins)]
     for n, o, i in zip(names, outs, ins):
         if o is not None:
@@ -582,12 +609,7 @@ def qk_rotary(rotary: Rotary, q, k, positions, q_norm=None, k_norm=None, eps: fl
     q, k: [B, N, H, D] bf16 views with one token stride, either may be None;
     positions: [N, axes] or [B, N, axes], int32 or float32; q_norm, k_norm:
     [D] bf16.  q_out may be q and k_out k (in place).  Returns (q_out, k_out)."""
-    given = _given(q, k)
-    if not given:
-        raise ValueError("qk_rotary: pass q, k or both")
-    for name, t in (("q", q), ("k", k)):
-        if t is not None:
-            _heads(name, t, given[0], rotary.head_dim)
+    given = _pair(("q", "k"), q, k, rotary.head_dim)
     B, N, H, D = given[0].shape
     dev = given[0].device
     pf, pb = _positions(rotary, given[0], positions)
@@ -607,12 +629,7 @@ def qk_rotary_backward(rotary: Rotary, dq, dk, positions, q=None, k=None, q_norm
     inputs, needed where there is a norm.  dq_out may be dq and dk_out dk.
     Returns (dq_out, dk_out, dq_norm, dk_norm); the norms' gradients are [D] fp32."""
     torch = _torch()
-    given = _given(dq, dk)
-    if not given:
-        raise ValueError("qk_rotary_backward: pass dq, dk or both")
-    for name, t in (("dq", dq), ("dk", dk)):
-        if t is not None:
-            _heads(name, t, given[0], rotary.head_dim)
+    given = _pair(("dq", "dk"), dq, dk, rotary.head_dim)
     B, N, H, D = given[0].shape
     dev = given[0].device
     pf, pb = _positions(rotary, given[0], positions)
@@ -642,6 +659,7 @@ def qk_rotary_backward(rotary: Rotary, dq, dk, positions, q=None, k=None, q_norm
 
 # ---------------------------------------------------------------- gated norm between blocks
 NORMS = {"layer": 0, "rms": 1}
+_I32S = ctypes.c_int32 * RC_MAX_SEGMENTS
 NormGrads = collections.namedtuple("NormGrads", "h x gate scale shift weight post_weight")
 
 
@@ -664,24 +682,20 @@ def _row_stride(name, t, like=None):
 
 def _norm_desc(h, spans, norm, post, eps, residual_scale, mods, weight, post_weight):
     """rc_norm of a call: shapes, spans and the strides that gate, scale and shift share."""
-    torch = _torch()
+    bf16, dev = _torch().bfloat16, h.device
     B, N, C = h.shape
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)}, got {norm!r}")
     spans = [(N, 0)] if spans is None else spans
     if len(spans) > RC_MAX_SEGMENTS:
         raise ValueError(f"at most {RC_MAX_SEGMENTS} spans")
-    d = rc_norm(B=B, C=C, norm=NORMS[norm], post=int(post), N=N, eps=eps, residual_scale=residual_scale,
-                n_spans=len(spans))
-    top = 0
-    for i, (n, g) in enumerate(spans):
-        d.rows[i], d.group[i] = n, g
-        top = max(top, g)
-    G, strides = top + 1, None
+    rows, groups = zip(*spans) if spans else ((), ())
+    G, strides = max(groups, default=0) + 1, None
+    mod_batch = mod_group = 0
     for name, t in mods:
         if t is None:
             continue
-        if t.dim() != 3 or t.dtype is not torch.bfloat16 or t.shape[0] != B or t.shape[2] != C or t.device != h.device:
+        if t.dim() != 3 or t.dtype is not bf16 or t.shape[0] != B or t.shape[2] != C or t.device != dev:
             raise ValueError(f"{name} must be a bf16 [{B}, groups, {C}] tensor on {h.device}, got {str(t.dtype)} "
                              f"{tuple(t.shape)} on {t.device}")
         if C > 1 and t.stride(2) != 1:
@@ -691,12 +705,13 @@ def _norm_desc(h, spans, norm, post, eps, residual_scale, mods, weight, post_wei
             raise ValueError("gate, scale and shift must share groups and strides (chunks of one tensor do)")
         strides = mine
     if strides is not None:
-        G, d.mod_batch, d.mod_group = strides
-    d.n_groups = G
-    for name, w in (("weight", weight), ("post_weight", post_weight)):
-        _norm_weight(name, w, C)
-    _same_device(h.device, weight=weight, post_weight=post_weight)
-    return d, G
+        G, mod_batch, mod_group = strides
+    if weight is not None or post_weight is not None:
+        for name, w in (("weight", weight), ("post_weight", post_weight)):
+            _norm_weight(name, w, C)
+        _same_device(h.device, weight=weight, post_weight=post_weight)
+    return rc_norm(B, C, G, NORMS[norm], post, N, eps, residual_scale, mod_batch, mod_group, len(rows),
+                   _I32S(*rows), _I32S(*groups)), G
 
 
 def gated_norm(h, x=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, norm: str = "layer",
@@ -720,13 +735,13 @@ def gated_norm(h, x=None, gate=None, scale=None, shift=None, weight=None, post_w
     if x is not None:
         ldx = _row_stride("x", x, h)
         if h_out is None:
-            h_out = _empty(tuple(h.shape), torch.bfloat16, dev, stream)
+            h_out = _empty(h.shape, torch.bfloat16, dev, stream)
         ldo = _row_stride("h_out", h_out, h)
     elif h_out is not None:
         raise ValueError("h_out is written only with x")
     if want_y:
         if y is None:
-            y = _empty(tuple(h.shape), torch.bfloat16, dev, stream)
+            y = _empty(h.shape, torch.bfloat16, dev, stream)
         ldy = _row_stride("y", y, h)
     elif y is not None:
         raise ValueError("y is written only with want_y")
@@ -754,11 +769,11 @@ def gated_norm_backward(dy, h, x=None, dh=None, gate=None, scale=None, shift=Non
     lddy = _row_stride("dy", dy, h) if dy is not None else 0
     lddh = _row_stride("dh", dh, h) if dh is not None else 0
     ldx = _row_stride("x", x, h) if x is not None else 0
-    dh_out = _empty(tuple(h.shape), torch.bfloat16, dev, stream) if dh_out is None else dh_out
+    dh_out = _empty(h.shape, torch.bfloat16, dev, stream) if dh_out is None else dh_out
     ldo = _row_stride("dh_out", dh_out, h)
     lddx = 0
     if x is not None:
-        dx = _empty(tuple(h.shape), torch.bfloat16, dev, stream) if dx is None else dx
+        dx = _empty(h.shape, torch.bfloat16, dev, stream) if dx is None else dx
         lddx = _row_stride("dx", dx, h)
     elif dx is not None:
         raise ValueError("dx is written only with x")

@@ -586,8 +586,8 @@ rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, con
 // Row groups per wave: whole tokens (their sines are computed once) as long as
 // that leaves 16 waves per CU, fewer for few tokens.
 int32_t rotary_groups(const RotaryParams& p, int32_t D) {
-  const int rows = (p.x[0] ? p.H : 0) + (p.x[1] ? p.H : 0), rw = 512 / D;
-  const int64_t all = (rows + rw - 1) / rw;
+  const int rw = 512 / D;
+  const int64_t all = int64_t(p.H + rw - 1) / rw * (p.x[0] && p.x[1] ? 2 : 1);
   const int64_t g = all * p.N * p.B / (16 * kCUs);
   return int32_t(std::max<int64_t>(1, std::min<int64_t>({g, all, 12})));
 }
@@ -659,9 +659,17 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   p.eps = d->eps;
   p.rscale = d->residual_scale;
   p.inv_c = 1.f / float(d->C);
-  // the backward's chunks: one work-group each, about one per CU, inside one span
+  // The backward's chunks, one work-group each and one work-group per CU:
+  // rows per chunk such that all of them fit one round (every span ends with a
+  // shorter one), a multiple of the four rows a work-group takes together.
   const int64_t rows = d->N * d->B;
-  p.chunk_rows = int32_t(std::max<int64_t>(8, (rows + kCUs - 1) / kCUs));
+  int64_t per = std::max<int64_t>(8, (rows + kCUs - 1) / kCUs + 3) / 4 * 4;
+  for (;; per += 4) {
+    int64_t n_chunks = 0;
+    for (int s = 0; s < p.n_spans; ++s) n_chunks += (p.span_rows[s] + per - 1) / per;
+    if (n_chunks * d->B <= kCUs || per >= rows) break;
+  }
+  p.chunk_rows = int32_t(per);
   for (int s = 0; s < p.n_spans; ++s) {
     p.span_chunk0[s] = p.chunks;
     p.chunks += (p.span_rows[s] + p.chunk_rows - 1) / p.chunk_rows;
@@ -1080,7 +1088,7 @@ rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, cons
   p.y_st = out_stride;
   p.sign = 1.f;
   p.groups = rotary_groups(p, D);
-  RC_TRY(check_blocks(B * N * ((2 * int64_t(H) * D + 511) / 512), "rotation"));
+  RC_TRY(check_blocks(B * N * ((int64_t(H) * D + 511) / 512 * 2), "rotation"));
   RC_TRY(check_launcher(launch_rotary, "rotation"));
   RC_TRY(hip_status(launch_rotary(p, D, stream), "rotation launch"));
   return RC_OK;
@@ -1129,7 +1137,7 @@ rc_status rc_qk_rotary_backward(const rc_rotary* R, int32_t B, int64_t N, int32_
   p.n_st = tok_stride;
   p.y_st = out_stride;
   p.sign = -1.f;
-  RC_TRY(check_blocks(B * N * ((2 * int64_t(H) * D + 511) / 512), "rotation gradient"));
+  RC_TRY(check_blocks(B * N * ((int64_t(H) * D + 511) / 512 * 2), "rotation gradient"));
   if (!norm) {
     if (N == 0) return RC_OK;
     p.groups = rotary_groups(p, D);

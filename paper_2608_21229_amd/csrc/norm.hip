@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "rc_lanes.h"
 #include "rc_layer.h"
 
 namespace rc {
@@ -21,12 +22,6 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = (__bf16)v[e];
   *reinterpret_cast<bf16x8*>(p) = o;
-}
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
-  return x;
 }
 
 // Sums over the T threads of a row.  Each array has two halves that take turns,
@@ -175,12 +170,13 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 // Backward: a work-group of NT threads takes one chunk of rows of one batch
 // entry and span, NT / T rows at a time, and leaves the chunk's sums over its
 // rows of dy, dy n and dh' x^ (the gradients of shift, scale and gate up to
-// factors of the column).
+// factors of the column).  The chunk's vectors (1 + scale) w and a gate w_p lie in
+// LDS; the next rows are loaded before the present ones are computed.
 template <int T, int GP, int NT>
 __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
   __shared__ RowSums<1> lds1;
   __shared__ RowSums<3> lds3;
-  extern __shared__ float acc_lds[];
+  __shared__ __attribute__((aligned(16))) float vec[2 * T * GP * 8];  // [2, C], at the end the row groups' sums
   constexpr int RB = NT / T;
   const int t = threadIdx.x % T, rb = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
   const int64_t b = blockIdx.x / p.chunks;
@@ -192,6 +188,47 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
   const int64_t row0 = b * p.N + p.span_row0[sp] + first;
   const int64_t mod = b * p.mod_sb + int64_t(p.span_group[sp]) * p.mod_sg;
   const int ng = p.C / 8;
+  bool has[GP];
+#pragma unroll
+  for (int i = 0; i < GP; ++i) has[i] = t + i * T < ng;
+
+  const bool dy_ = p.dy.p != nullptr, dh_ = p.dh.p != nullptr, x_ = p.x.p != nullptr;
+  bf16x8 ry[GP], rn[GP], rh[GP], rx[GP];  // the rows of the next step
+  const auto load_rows = [&](int i0) {
+    const int64_t r = row0 + min(i0 + rb, count - 1);
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      const int c = (t + i * T) * 8;
+      ry[i] = rn[i] = rh[i] = rx[i] = bf16x8{};
+      if (!has[i]) continue;
+      if (dy_) {
+        rn[i] = load8(p.h.p + r * p.h.ld + c);
+        ry[i] = load8(p.dy.p + r * p.dy.ld + c);
+      }
+      if (dh_) rh[i] = load8(p.dh.p + r * p.dh.ld + c);
+      if (x_) rx[i] = load8(p.x.p + r * p.x.ld + c);
+    }
+  };
+  load_rows(0);
+  for (int g = threadIdx.x; g < ng; g += NT) {
+    float s[8], a[8];
+    const bf16x8 vs = p.scale ? load8(p.scale + mod + g * 8) : bf16x8{};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = 1.f + float(vs[e]), a[e] = p.rscale;
+    const auto times = [&](float (&v)[8], const uint16_t* w) {
+      if (!w) return;
+      const bf16x8 x = load8(w + g * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= float(x[e]);
+    };
+    times(s, p.weight);
+    times(a, p.gate ? p.gate + mod : nullptr);
+    times(a, p.post_weight);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) vec[g * 8 + e] = s[e], vec[p.C + g * 8 + e] = a[e];
+  }
+  __syncthreads();
+
   int half1 = 0, half3 = 0;
   float a_shift[GP][8], a_scale[GP][8], a_gate[GP][8];
 #pragma unroll
@@ -200,116 +237,93 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
     for (int e = 0; e < 8; ++e) a_shift[i][e] = a_scale[i][e] = a_gate[i][e] = 0.f;
   for (int i0 = 0; i0 < count; i0 += RB) {
     const bool in = i0 + rb < count;
-    const int64_t r = row0 + (in ? i0 + rb : 0);
+    const int64_t r = row0 + i0 + rb;
     float n[GP][8], d[GP][8], dh[GP][8];
+    bf16x8 cx[GP];
     float m[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
-      const int g = t + i * T;
-      const bool has = g < ng && in;
-      const bf16x8 a = p.dh.p && has ? load8(p.dh.p + r * p.dh.ld + g * 8) : bf16x8{};
+      cx[i] = rx[i];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dh[i][e] = float(a[e]);
-    }
-    if (p.dy.p) {
-#pragma unroll
-      for (int i = 0; i < GP; ++i) {
-        const int g = t + i * T;
-        const bool has = g < ng && in;
-        const bf16x8 a = has ? load8(p.h.p + r * p.h.ld + g * 8) : bf16x8{};
-        const bf16x8 c = has ? load8(p.dy.p + r * p.dy.ld + g * 8) : bf16x8{};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          n[i][e] = float(a[e]);
-          d[i][e] = float(c[e]);
-          m[0] += n[i][e];
-        }
+      for (int e = 0; e < 8; ++e) {
+        n[i][e] = float(rn[i][e]);
+        d[i][e] = float(ry[i][e]);
+        dh[i][e] = float(rh[i][e]);
+        m[0] += n[i][e];
       }
+    }
+    if (i0 + RB < count) load_rows(i0 + RB);
+    if (dy_) {
       if (!p.rms) {
         row_sums<T, 1>(m, lds1, rb, half1);
         const float mean = m[0] * p.inv_c;
 #pragma unroll
-        for (int i = 0; i < GP; ++i) {
-          if (t + i * T >= ng || !in) continue;
+        for (int i = 0; i < GP; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) n[i][e] -= mean;
-        }
+          for (int e = 0; e < 8; ++e) n[i][e] = has[i] ? n[i][e] - mean : 0.f;
       }
       // over the row: n^2, dn, dn n (dn = dy (1 + scale) w)
       float k[3] = {0.f, 0.f, 0.f};
-      float dn[GP][8];
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const int g = t + i * T;
-        bf16x8 ws{}, ww{};
-        if (p.scale && g < ng) ws = load8(p.scale + mod + g * 8);
-        if (p.weight && g < ng) ww = load8(p.weight + g * 8);
+        const float* w = vec + (has[i] ? (t + i * T) * 8 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float x = d[i][e] + d[i][e] * float(ws[e]);
-          if (p.weight) x *= float(ww[e]);
-          dn[i][e] = x;
+          const float dn = d[i][e] * w[e];
           k[0] += n[i][e] * n[i][e];
-          k[1] += x;
-          k[2] += x * n[i][e];
+          k[1] += dn;
+          k[2] += dn * n[i][e];
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
       const float rs = rsqrtf(k[0] * p.inv_c + p.eps);
       const float mean = p.rms ? 0.f : k[1] * p.inv_c, dot = k[2] * p.inv_c * rs * rs;
+      const float on = in ? 1.f : 0.f, rin = in ? rs : 0.f;
 #pragma unroll
-      for (int i = 0; i < GP; ++i)
+      for (int i = 0; i < GP; ++i) {
+        const float* w = vec + (has[i] ? (t + i * T) * 8 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          a_shift[i][e] += d[i][e];
-          a_scale[i][e] += d[i][e] * n[i][e] * rs;
-          dh[i][e] += rs * (dn[i][e] - mean - n[i][e] * dot);
+          a_shift[i][e] += d[i][e] * on;
+          a_scale[i][e] += d[i][e] * (n[i][e] * rin);
+          dh[i][e] += rs * (d[i][e] * w[e] - mean - n[i][e] * dot);
         }
+      }
     }
     if (in) {
 #pragma unroll
-      for (int i = 0; i < GP; ++i) {
-        const int g = t + i * T;
-        if (g < ng) store8(p.dh_in.p + r * p.dh_in.ld + g * 8, dh[i]);
-      }
+      for (int i = 0; i < GP; ++i)
+        if (has[i]) store8(p.dh_in.p + r * p.dh_in.ld + (t + i * T) * 8, dh[i]);
     }
-    if (!p.x.p) continue;
-    float x[GP][8], k[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < GP; ++i) {
-      const int g = t + i * T;
-      const bool has = g < ng && in;
-      const bf16x8 a = has ? load8(p.x.p + r * p.x.ld + g * 8) : bf16x8{};
-      bf16x8 wg{}, ww{};
-      if (p.gate && g < ng) wg = load8(p.gate + mod + g * 8);
-      if (p.post_weight && g < ng) ww = load8(p.post_weight + g * 8);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[i][e] = float(a[e]);
-        float du = p.rscale * dh[i][e];
-        d[i][e] = has ? du : 0.f;
-        if (p.gate) du *= float(wg[e]);
-        if (p.post_weight) du *= float(ww[e]);
-        dh[i][e] = du;
-        k[0] += x[i][e] * x[i][e];
-        k[1] += du * x[i][e];
-      }
-    }
-    float rx = 1.f, dot = 0.f;
+    if (!x_) continue;
+    float k[3] = {0.f, 0.f, 0.f}, rq = 1.f, dot = 0.f;
     if (p.post) {
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const float* w = vec + p.C + (has[i] ? (t + i * T) * 8 : 0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = float(cx[i][e]);
+          k[0] += x * x;
+          k[1] += dh[i][e] * w[e] * x;
+        }
+      }
       row_sums<T, 3>(k, lds3, rb, half3);
-      rx = rsqrtf(k[0] * p.inv_c + p.eps);
-      dot = k[1] * p.inv_c * rx * rx;
+      rq = rsqrtf(k[0] * p.inv_c + p.eps);
+      dot = k[1] * p.inv_c * rq * rq;
     }
+    const float gin = in ? rq * p.rscale : 0.f;
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
-      const int g = t + i * T;
+      const float* w = vec + p.C + (has[i] ? (t + i * T) * 8 : 0);
+      float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        a_gate[i][e] += d[i][e] * x[i][e] * rx;
-        dh[i][e] = rx * (dh[i][e] - x[i][e] * dot);
+        const float x = float(cx[i][e]);
+        a_gate[i][e] += dh[i][e] * (x * gin);
+        o[e] = rq * (dh[i][e] * w[e] - x * dot);
       }
-      if (in && g < ng) store8(p.dx.p + r * p.dx.ld + g * 8, dh[i]);
+      if (in && has[i]) store8(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
     }
   }
   // the row groups' sums, in order, through LDS
@@ -318,73 +332,85 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
   for (int q = 0; q < 3; ++q) {
     auto& a = q == 0 ? a_shift : q == 1 ? a_scale : a_gate;
     if constexpr (RB > 1) {
-      __syncthreads();
       for (int w = 0; w < RB; ++w) {
+        __syncthreads();
         if (rb == w) {
 #pragma unroll
           for (int i = 0; i < GP; ++i) {
-            const int g = t + i * T;
-            if (g < ng)
+            if (!has[i]) continue;
+            float* at = vec + (t + i * T) * 8;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) acc_lds[g * 8 + e] = w == 0 ? a[i][e] : acc_lds[g * 8 + e] + a[i][e];
+            for (int e = 0; e < 8; ++e) at[e] = w == 0 ? a[i][e] : at[e] + a[i][e];
           }
         }
-        __syncthreads();
       }
-      for (int c = threadIdx.x; c < p.C; c += NT) out[q * p.C + c] = acc_lds[c];
+      __syncthreads();
+      for (int c = threadIdx.x; c < p.C; c += NT) out[q * p.C + c] = vec[c];
     } else {
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const int g = t + i * T;
-        if (g < ng)
+        if (!has[i]) continue;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) out[q * p.C + g * 8 + e] = a[i][e];
+        for (int e = 0; e < 8; ++e) out[q * p.C + (t + i * T) * 8 + e] = a[i][e];
       }
     }
   }
 }
 
-// The gradients shared between rows from the chunks' sums: 64 columns per
-// work-group, each of its 16 waves a share of the chunks.
+// The gradients shared between rows from the chunks' sums.  Work-group (x, y):
+// 64 columns, a wave per 16th of the chunks; y < B G: shift, scale and gate of a
+// batch entry and group; the last y: the weights, over all of them.
 __global__ __launch_bounds__(1024) void norm_shared_kernel(const NormParams p) {
   __shared__ float part[16][3][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   const bool in = c < p.C;
-  float dw = 0.f, dwp = 0.f;
   const auto bf = [&](const uint16_t* v, int64_t at) { return __uint_as_float(uint32_t(v[at]) << 16); };
-  for (int b = 0; b < p.B; ++b)
-    for (int g = 0; g < p.G; ++g) {
+  const int one = int(blockIdx.y), all = p.B * p.G;
+  float sum[3] = {0.f, 0.f, 0.f};
+  for (int b = one < all ? one / p.G : 0; b < (one < all ? one / p.G + 1 : p.B) && in; ++b)
+    for (int s = 0; s < p.n_spans; ++s) {
+      const int g = p.span_group[s];
+      if (one < all && g != one % p.G) continue;
+      const int end = s + 1 < p.n_spans ? p.span_chunk0[s + 1] : p.chunks;
       float a[3] = {0.f, 0.f, 0.f};
-      for (int s = 0; s < p.n_spans; ++s) {
-        if (p.span_group[s] != g) continue;
-        const int end = s + 1 < p.n_spans ? p.span_chunk0[s + 1] : p.chunks;
-        for (int k = p.span_chunk0[s] + wave; k < end && in; k += 16) {
-          const float* q = p.partial + (int64_t(b) * p.chunks + k) * 3 * p.C + c;
-          a[0] += q[0];
-          a[1] += q[p.C];
-          a[2] += q[2 * int64_t(p.C)];
+      const float* q = p.partial + int64_t(b) * p.chunks * 3 * p.C + c;
+      for (int k0 = p.span_chunk0[s] + wave; k0 < end; k0 += 64) {
+        float v[4][3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = k0 + 16 * j;
+#pragma unroll
+          for (int i = 0; i < 3; ++i) v[j][i] = k < end ? q[(int64_t(k) * 3 + i) * p.C] : 0.f;
         }
-      }
-      __syncthreads();
 #pragma unroll
-      for (int q = 0; q < 3; ++q) part[wave][q][lane] = a[q];
-      __syncthreads();
-      if (wave != 0 || !in) continue;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        a[q] = 0.f;
-        for (int w = 0; w < 16; ++w) a[q] += part[w][q][lane];
+          for (int i = 0; i < 3; ++i) a[i] += v[j][i];
       }
-      const int64_t mod = b * p.mod_sb + int64_t(g) * p.mod_sg + c, at = (int64_t(b) * p.G + g) * p.C + c;
-      if (p.dshift) p.dshift[at] = a[0];
-      if (p.dscale) p.dscale[at] = a[1] * (p.weight ? bf(p.weight, c) : 1.f);
-      if (p.dgate) p.dgate[at] = a[2] * (p.post_weight ? bf(p.post_weight, c) : 1.f);
-      dw += a[1] * (p.scale ? 1.f + bf(p.scale, mod) : 1.f);
-      dwp += a[2] * (p.gate ? bf(p.gate, mod) : 1.f);
+      const int64_t mod = b * p.mod_sb + int64_t(g) * p.mod_sg + c;
+      if (one == all) {
+        if (p.scale) a[1] *= 1.f + bf(p.scale, mod);
+        if (p.gate) a[2] *= bf(p.gate, mod);
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) sum[i] += a[i];
     }
-  if (wave != 0 || !in) return;
-  if (p.dweight) p.dweight[c] = dw;
-  if (p.dpost_weight) p.dpost_weight[c] = dwp;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) part[wave][i][lane] = sum[i];
+  __syncthreads();
+  if (wave > 2 || !in) return;  // a wave per sum
+  float x = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) x += part[w][wave][lane];
+  const int64_t at = int64_t(one) * p.C + c;
+  if (one == all) {
+    if (wave == 1 && p.dweight) p.dweight[c] = x;
+    if (wave == 2 && p.dpost_weight) p.dpost_weight[c] = x;
+    return;
+  }
+  if (wave == 0 && p.dshift) p.dshift[at] = x;
+  if (wave == 1 && p.dscale) p.dscale[at] = x * (p.weight ? bf(p.weight, c) : 1.f);
+  if (wave == 2 && p.dgate) p.dgate[at] = x * (p.post_weight ? bf(p.post_weight, c) : 1.f);
 }
 
 template <int T, int GP>
@@ -396,9 +422,11 @@ template <int T, int GP>
 void launch_bwd(const NormParams& p, hipStream_t s) {
   constexpr int NT = 512;
   if (p.chunks > 0)
-    hipLaunchKernelGGL((norm_backward_kernel<T, GP, NT>), dim3(int64_t(p.B) * p.chunks), dim3(NT),
-                       NT > T ? p.C * sizeof(float) : 0, s, p);
-  hipLaunchKernelGGL(norm_shared_kernel, dim3((p.C + 63) / 64), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((norm_backward_kernel<T, GP, NT>), dim3(int64_t(p.B) * p.chunks), dim3(NT), 0,
+                       s, p);
+  const int weights = p.dweight || p.dpost_weight, vectors = p.dshift || p.dscale || p.dgate;
+  if (weights || vectors)
+    hipLaunchKernelGGL(norm_shared_kernel, dim3((p.C + 63) / 64, p.B * p.G + weights), dim3(1024), 0, s, p);
 }
 
 }  // namespace

@@ -70,7 +70,7 @@ struct RotaryParams {
 };
 int launch_rotary(const RotaryParams& p, int D, void* stream) RC_WEAK;
 int launch_rotary_norm_backward(const RotaryParams& p, int D, void* stream) RC_WEAK;
-constexpr int kRotaryBlocks = 1024;  // work-groups of the backward with a norm, at most
+constexpr int kRotaryBlocks = 768;  // work-groups of the backward with a norm, at most (three per CU)
 
 // ---------------------------------------------------------------- gated norm
 struct NormRows {  // [B * N, C] rows
