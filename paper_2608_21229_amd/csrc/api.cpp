@@ -474,12 +474,13 @@ rc_layout key_layout(const rc_layout* L) {
   return t;
 }
 
-// The schedule of the attention gradient, from the plans of full recomputes of
-// the layout and of its keys.
-rc_status plan_bwd(const rc_layout* L, BwdParams& b) {
+// The schedule of the attention gradient for bh (batch, head)s, from the plans of
+// full recomputes of the layout and of its keys.
+rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
   const rc_layout kl = key_layout(L);
-  int64_t cost[2 * RC_MAX_SEGMENTS];
-  BwdSeg seg[2 * RC_MAX_SEGMENTS];
+  constexpr int kMax = 2 * RC_MAX_SEGMENTS;
+  BwdSeg seg[kMax];
+  int64_t tiles[kMax], count[kMax];  // streamed tiles of an own tile, own tiles over all heads
   int n = 0;
   for (int keys = 0; keys < 2; ++keys) {
     Params p;
@@ -498,25 +499,66 @@ rc_status plan_bwd(const rc_layout* L, BwdParams& b) {
         last->len += q.len;
         continue;
       }
-      // a tile of keys takes about 6 / 5 of the time of a tile of queries
-      cost[n] = int64_t(q.ktiles) * (keys ? 6 : 5);
-      seg[n++] = BwdSeg{q.row0, q.len, 0, keys * kMaxRanges + q.r0, q.nr, keys};
+      tiles[n] = q.ktiles;
+      seg[n++] = BwdSeg{q.row0, q.len, 0, keys * kMaxRanges + q.r0, q.nr, keys, 1, 0};
     }
+  }
+  // Pieces of a tile's streamed rows, so that few heads fill the chip: of at
+  // most `most` tiles each.  Costs in fifths of a tile of queries' time (a tile of
+  // keys takes six); a piece costs two tiles besides (own rows, first loads,
+  // stores); the launch ends with its longest piece, or with the work spread
+  // over the CUs and a part of a piece.  A split costs the merge's launch and the
+  // partials (one of 128 KB, written and read, is 9 hundredths).
+  int64_t longest = 1;
+  for (int i = 0; i < n; ++i) {
+    count[i] = bh * ((seg[i].len + kBwdOwn - 1) / kBwdOwn);
+    longest = std::max(longest, tiles[i]);
+  }
+  const auto splits_of = [&](int i, int64_t most) { return std::max<int64_t>(1, (tiles[i] + most - 1) / most); };
+  const auto cost_of = [&](int i, int64_t most) {
+    const int64_t s = splits_of(i, most);
+    return ((tiles[i] + s - 1) / s + 2) * (seg[i].keys ? 6 : 5);
+  };
+  int64_t best = INT64_MAX, best_most = longest;
+  for (int64_t s = 1; s <= 32 && (s == 1 || (longest + s - 1) / s >= 4); ++s) {
+    const int64_t most = (longest + s - 1) / s;
+    int64_t top = 0, total = 0, slots = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t k = splits_of(i, most), c = cost_of(i, most);
+      top = std::max(top, c);
+      total += count[i] * k * c;
+      if (k > 1) slots += count[i] * k * (1 + seg[i].keys);
+    }
+    int64_t est = std::max(top, total / kCUs + top / 3);
+    if (s > 1) est += 10 + slots * 9 / 100;
+    if (s == 1 ? true : est * 10 < best * 9 || (best_most < longest && est < best)) best = est, best_most = most;
   }
   // Work-groups run in this order: the longest first, so that the launch ends
   // with short ones (in the order of the segments, queries after keys: 512-pixel
   // edit 348 us, longest first 324).
-  int order[2 * RC_MAX_SEGMENTS];
+  int order[kMax];
   for (int i = 0; i < n; ++i) order[i] = i;
-  std::stable_sort(order, order + n, [&](int x, int y) { return cost[x] > cost[y]; });
+  std::sort(order, order + n, [&](int x, int y) {
+    const int64_t cx = cost_of(x, best_most), cy = cost_of(y, best_most);
+    return cx != cy ? cx > cy : x < y;
+  });
   b.n_seg = n;
-  b.n_tiles = 0;
+  b.n_pieces = b.n_slots = 0;
   for (int i = 0; i < n; ++i) {
-    b.seg[i] = seg[order[i]];
-    b.seg[i].tile0 = b.n_tiles;
-    b.n_tiles += (b.seg[i].len + kBwdOwn - 1) / kBwdOwn;
+    BwdSeg& g = b.seg[i];
+    g = seg[order[i]];
+    const int own = (g.len + kBwdOwn - 1) / kBwdOwn;
+    g.splits = int32_t(splits_of(order[i], best_most));
+    g.piece0 = b.n_pieces;
+    b.n_pieces += own * g.splits;
+    g.slot0 = b.n_slots;
+    if (g.splits > 1) b.n_slots += own * g.splits * (1 + g.keys);
   }
   return RC_OK;
+}
+
+size_t bwd_partial_bytes(const BwdParams& p, int64_t bh, int32_t D) {
+  return size_t(bh) * p.n_slots * kBwdOwn * D * sizeof(float);
 }
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
@@ -959,7 +1001,10 @@ rc_status rc_linear(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda,
 size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D) {
   if (B < 1 || H < 1 || B > 65535 || H > 65535 || (D != 64 && D != 128)) return 0;
   if (check_layout(L, RC_ENTRY_FULL) != RC_OK) return 0;
-  return 2 * bwd_row_bytes(int64_t(B) * H * count_rows(L, RowSet::All));
+  BwdParams p;
+  const int64_t bh = int64_t(B) * H;
+  if (plan_bwd(L, bh, p) != RC_OK) return 0;
+  return 2 * bwd_row_bytes(bh * count_rows(L, RowSet::All)) + bwd_partial_bytes(p, bh, D);
 }
 
 rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, int32_t D, float scale, const void* q,
@@ -988,10 +1033,10 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   const int64_t n = count_rows(L, RowSet::All), rows = int64_t(B) * H * n;
   BwdParams p;
   memset(&p, 0, sizeof p);
-  RC_TRY(plan_bwd(L, p));
-  RC_TRY(check_blocks(int64_t(B) * H * p.n_tiles, "attention gradient"));
+  RC_TRY(plan_bwd(L, int64_t(B) * H, p));
+  RC_TRY(check_blocks(int64_t(B) * H * p.n_pieces, "attention gradient"));
   RC_TRY(check_blocks((rows * (D / 8) + 255) / 256, "attention gradient"));
-  const size_t need = 2 * bwd_row_bytes(rows);
+  const size_t need = 2 * bwd_row_bytes(rows) + bwd_partial_bytes(p, int64_t(B) * H, D);
   if (!workspace || !aligned16(workspace) || ws_bytes < need) {
     set_error("the attention gradient needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
               workspace ? ws_bytes : size_t(0));
@@ -1010,6 +1055,7 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   p.dv = static_cast<uint16_t*>(dv);
   p.nlse = static_cast<float*>(workspace);
   p.ndelta = p.nlse + bwd_row_bytes(rows) / sizeof(float);
+  p.partial = p.ndelta + bwd_row_bytes(rows) / sizeof(float);
   p.st = tok_stride;
   p.g_st = grad_stride;
   p.B = B;

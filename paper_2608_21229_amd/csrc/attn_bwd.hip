@@ -75,14 +75,32 @@ __device__ __forceinline__ int swz(int row) {
   return ((row & 2) << 1) | ((row >> 1) & 2) | ((row >> 3) & 1);
 }
 
+// One 32 x 32 block of an output: the lane of half hh holds columns 8 (r / 4) + 4
+// hh + r % 4 of its row.  The halves trade registers, so that a lane owns eight
+// consecutive columns of each 16 and stores 16 bytes.
+__device__ __forceinline__ void store_block(uint16_t* out, const f32x16& acc, float f, bool in) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * i + e] * f),
+                                                      __float_as_uint(acc[8 * i + 4 + e] * f), false, false);
+      o[e] = (__bf16)__uint_as_float(x[0]);
+      o[4 + e] = (__bf16)__uint_as_float(x[1]);
+    }
+    if (in) *reinterpret_cast<bf16x8*>(out + 16 * i) = o;
+  }
+}
+
 template <int D, bool KV, int NB, int NW, int ST>
-__device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const BwdSeg seg, int bh, int t) {
+__device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const BwdSeg seg, int bh, int t, int piece) {
   using T = Bwd<D, KV, NB, NW, ST>;
   constexpr int PF = D == 64 ? 3 : 2;  // fragments read ahead of their MFMAs
   constexpr int GR = T::GR, DC = T::DC, DB = T::DB, kT = T::kT;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = bh / p.H, h = bh % p.H;
+  const int b = __builtin_amdgcn_readfirstlane(bh / p.H), h = bh - b * p.H;
   const int own0 = t * T::kOwn + wave * 32 * NB;  // inside the segment
 
   const int64_t o_st = int64_t(p.H) * D;
@@ -133,34 +151,48 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   // range table is read again only at a range's end.
   int n_tiles = 0;
   for (int i = 0; i < seg.nr; ++i) n_tiles += (p.range[seg.r0 + i].len + kTile - 1) / kTile;
+  int skip = int(int64_t(n_tiles) * piece / seg.splits);  // tiles of the pieces before
+  n_tiles = int(int64_t(n_tiles) * (piece + 1) / seg.splits) - skip;
   int ir = seg.r0, rem = 0;
+  for (; ir + 1 < seg.r0 + seg.nr; ++ir) {
+    const int n = (p.range[ir].len + kTile - 1) / kTile;
+    if (skip < n) break;
+    skip -= n;
+  }
+  int left = n_tiles;  // tiles to load
   const uint16_t *l1 = y1, *l2 = y2;
   const float* ls = ((wave & 1) ? p.ndelta : p.nlse) + s_base;
-  const auto load_range = [&] {
+  const auto load_range = [&](int tile) {
     const BwdRange rg = p.range[ir];
-    l1 = y1 + uniform(rg.start * y1_st);
-    l2 = y2 + uniform(rg.start * y2_st);
-    ls = ((wave & 1) ? p.ndelta : p.nlse) + s_base + rg.start;
-    rem = rg.len;
+    const int64_t row = rg.start + int64_t(tile) * kTile;
+    l1 = y1 + uniform(row * y1_st);
+    l2 = y2 + uniform(row * y2_st);
+    ls = ((wave & 1) ? p.ndelta : p.nlse) + s_base + row;
+    rem = rg.len - tile * kTile;
   };
   const auto advance = [&] {
     rem -= kTile;
-    if (rem > 0) {
+    if (--left <= 0) {  // past the piece: the ring's last loads bring zeros
+      rem = 0;
+    } else if (rem > 0) {
       l1 += kTile * y1_st;
       l2 += kTile * y2_st;
       ls += kTile;
-    } else if (++ir < seg.r0 + seg.nr) {
-      load_range();
     } else {
-      rem = 0;
+      ++ir;
+      load_range(0);
     }
   };
-  if (seg.nr > 0) load_range();
+  if (n_tiles > 0) load_range(skip);
   const uint32_t lds0 = lds_u32(ring) + wave * 1024;
-  const int row_l = wave * (512 / D) + lane / GR;
-  const uint32_t gran = uint32_t((lane % GR) ^ swz<D>(row_l)) * 16;
-  const uint32_t voff1 = uint32_t(row_l) * uint32_t(y1_st * 2) + gran;
-  const uint32_t voff2 = uint32_t(row_l) * uint32_t(y2_st * 2) + gran;
+  // a lane's byte offsets in the tiles of Y1 and Y2, computed where a tile is loaded (fresh_lane)
+  uint32_t voff1 = 0, voff2 = 0;
+  const auto lane_offsets = [&] {
+    const int l = int(fresh_lane()), row = wave * (512 / D) + l / GR;
+    const uint32_t gran = uint32_t((l % GR) ^ swz<D>(row)) * 16;
+    voff1 = uint32_t(row) * uint32_t(y1_st * 2) + gran;
+    voff2 = uint32_t(row) * uint32_t(y2_st * 2) + gran;
+  };
   // a wave's chunks lie a multiple of 16 rows apart, so their lane offsets are the same
   constexpr int CH = kT / 1024 / NW, kStep = 1024 * NW / (D * 2);
   static_assert(kStep % 16 == 0, "one swizzle for a wave's chunks");
@@ -187,6 +219,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   };
   const auto issue = [&](uint32_t stage) {
     start_tile();
+    lane_offsets();
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) issue1(stage, l);
   };
@@ -203,10 +236,10 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   // + hh and d block d are the base XOR a constant, since a stage starts at a
   // multiple of 1 KB.
   const int li = lane & 15;
-  const uint32_t fk = lds_u32(ring) + (lane & 31) * D * 2 + 16 * (swz<D>(lane & 31) ^ hh);
+  uint32_t kc = lds_u32(ring) + (lane & 31) * D * 2 + 16 * (swz<D>(lane & 31) ^ hh);
   const int gc = 2 * ((lane >> 4) & 1) + ((li & 3) >> 1);
   const int r0 = 4 * hh + (li >> 2);
-  const uint32_t v0 = lds_u32(ring) + r0 * D * 2 + 16 * (gc ^ swz<D>(r0)) + 8 * (li & 1);
+  uint32_t t0 = lds_u32(ring) + r0 * D * 2 + 16 * (gc ^ swz<D>(r0)) + 8 * (li & 1);
   constexpr uint32_t k8 = 16 * (D == 128 ? 2 : 1);  // 8 rows further the slot differs in this bit
   const auto rd = [](uint32_t base, int c, int off) {
     return *reinterpret_cast<lds_cbf16x8*>((base ^ uint32_t(32 * c)) + uint32_t(off));
@@ -289,7 +322,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
     start(s, nl);
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
-      const bf16x8 a = rd(fk, c, 0);
+      const bf16x8 a = rd(kc, c, 0);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) s[nb] = mm(a, f1[nb][c], s[nb]);
     }
@@ -298,15 +331,15 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 #pragma unroll
     for (int e = 0; e < kE1; ++e) unit(e);
 #pragma unroll
-    for (int g = 0; g < PF; ++g) fr[g] = rd(fk, g, kT);
+    for (int g = 0; g < PF; ++g) fr[g] = rd(kc, g, kT);
   }
   for (int tile = 0; tile < n_tiles; ++tile) {
-    uint32_t kc = fk + cur, t0 = v0 + cur;
+    const uint32_t step = nxt - cur;  // to the next stage
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       // at D = 128 the registers are full: addresses are recomputed (one XOR a read), not kept
       if constexpr (D == 128) asm volatile("" : "+v"(kc), "+v"(t0));
-      const uint32_t kn = j == 0 ? kc : fk + nxt;       // the next sub-block: rows, statistics
+      const uint32_t kn = j == 0 ? kc : kc + step;      // the next sub-block: rows, statistics
       const uint32_t sn = j == 0 ? cur : nxt;
       constexpr int kSub = 32 * D * 2;
       const int here = j * kSub, there = j == 0 ? kSub : 0, sthere = j == 0 ? 128 : 0;
@@ -389,6 +422,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV) ds(8, 16, 2 * c + nb, DC);
           else ds(0, 16, 2 * c + nb - 2, 2 * DC - 2);
+          
           fence();
         }
       }
@@ -425,6 +459,8 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
       for (int i = 0; i < PF; ++i) fr[i] = first[i];
     }
     advance();
+    kc += step;
+    t0 += step;
     cur = nxt;
     nxt = nxt + T::kStage == ST * T::kStage ? 0 : nxt + T::kStage;
     fill = fill + T::kStage == ST * T::kStage ? 0 : fill + T::kStage;
@@ -442,30 +478,38 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
       if constexpr (KV) settle(acc2[nb][d]);
     }
 
-  const auto store = [&](uint16_t* out, const f32x16& acc, int nb, int d, float f) {
-    const int r = own0 + nb * 32 + (lane & 31);
+  const int lane_ = int(fresh_lane());
+  if (seg.splits > 1) {  // a partial: 1 KB runs, in accumulator order
+    const int own_tiles = (seg.len + kBwdOwn - 1) / kBwdOwn;
+    const int64_t slot = int64_t(p.B) * p.H * seg.slot0 +
+                         ((int64_t(bh) * own_tiles + t) * seg.splits + piece) * (KV ? 2 : 1);
+    f32x4* out = reinterpret_cast<f32x4*>(p.partial + slot * kBwdOwn * D) + lane_;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      bf16x8 o;
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * i + e] * f),
-                                                        __float_as_uint(acc[8 * i + 4 + e] * f), false, false);
-        o[e] = (__bf16)__uint_as_float(x[0]);
-        o[4 + e] = (__bf16)__uint_as_float(x[1]);
-      }
-      if (r < seg.len)
-        *reinterpret_cast<bf16x8*>(out + (int64_t(b) * p.n_rows + seg.row0 + r) * p.g_st + int64_t(h) * D + d * 32 +
-                                   16 * i + 8 * hh) = o;
-    }
-  };
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
+        for (int i = 0; i < 4; ++i) {
+          const int at = (((wave * NB + nb) * DB + d) * 4 + i) * 64;
+          const f32x16& a = acc1[nb][d];
+          out[at] = f32x4{a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3]};
+          if constexpr (KV) {
+            const f32x16& c = acc2[nb][d];
+            out[at + kBwdOwn * D / 4] = f32x4{c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]};
+          }
+        }
+    return;
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = own0 + nb * 32 + (lane_ & 31);
+    const int64_t at = (int64_t(b) * p.n_rows + seg.row0 + r) * p.g_st + int64_t(h) * D + 8 * (lane_ >> 5);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      store(KV ? p.dk : p.dq, acc1[nb][d], nb, d, p.scale);
-      if constexpr (KV) store(p.dv, acc2[nb][d], nb, d, 1.f);
+      store_block((KV ? p.dk : p.dq) + at + d * 32, acc1[nb][d], p.scale, r < seg.len);
+      if constexpr (KV) store_block(p.dv + at + d * 32, acc2[nb][d], 1.f, r < seg.len);
     }
+  }
 }
 
 template <int D, int NB, int NW, int ST>
@@ -481,12 +525,61 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
   const int hx = split ? bhs / 8 : bhs;
   const int w = split ? blockIdx.x >> 3 : blockIdx.x;
   int si = 0;
-  while (si + 1 < p.n_seg && p.seg[si + 1].tile0 * hx <= w) ++si;
+  while (si + 1 < p.n_seg && p.seg[si + 1].piece0 * hx <= w) ++si;
   const BwdSeg seg = p.seg[si];
-  const int in_seg = w - seg.tile0 * hx, seg_tiles = (seg.len + kBwdOwn - 1) / kBwdOwn;
-  const int bh = (split ? (blockIdx.x & 7) * hx : 0) + in_seg / seg_tiles, t = in_seg % seg_tiles;
-  if (seg.keys) bwd_tile<D, true, NB, NW, ST>(p, ring, seg, bh, t);
-  else bwd_tile<D, false, NB, NW, ST>(p, ring, seg, bh, t);
+  const int in_seg = w - seg.piece0 * hx, pieces = (seg.len + kBwdOwn - 1) / kBwdOwn * seg.splits;
+  // (quotients come from vector instructions; as scalars they take no registers across the loops)
+  const int head = __builtin_amdgcn_readfirstlane(in_seg / pieces), in_head = in_seg - head * pieces;
+  const int t = __builtin_amdgcn_readfirstlane(in_head / seg.splits), piece = in_head - t * seg.splits;
+  const int bh = (split ? (blockIdx.x & 7) * hx : 0) + head;
+  if (seg.keys) bwd_tile<D, true, NB, NW, ST>(p, ring, seg, bh, t, piece);
+  else bwd_tile<D, false, NB, NW, ST>(p, ring, seg, bh, t, piece);
+}
+
+// The pieces of split tiles, summed in order.  A wave takes one 32 x 32 block; its
+// partials' loads are in flight together, four pieces at a time.
+template <int D>
+__global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) {
+  constexpr int DB = D / 32, kBlocks = kBwdOwn / 32 * DB;  // blocks of one output of a tile
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  int64_t w = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t bhs = int64_t(p.B) * p.H;
+  int si = 0;
+  int64_t own = 0;
+  for (; si < p.n_seg; ++si) {
+    if (p.seg[si].splits <= 1) continue;
+    own = (p.seg[si].len + kBwdOwn - 1) / kBwdOwn;
+    const int64_t n = bhs * own * (1 + p.seg[si].keys) * kBlocks;
+    if (w < n) break;
+    w -= n;
+  }
+  if (si == p.n_seg) return;
+  const BwdSeg seg = p.seg[si];
+  const int outs = 1 + seg.keys;
+  const int block = int(w % kBlocks), out = int(w / kBlocks % outs);
+  const int64_t tile = w / kBlocks / outs;  // (batch, head), own tile
+  const f32x4* src = reinterpret_cast<const f32x4*>(p.partial + (bhs * seg.slot0 + tile * seg.splits * outs + out) * kBwdOwn * D) +
+                     block * 256 + lane;
+  f32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  for (int s0 = 0; s0 < seg.splits; s0 += 4) {
+    f32x4 v[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[j][i] = s0 + j < seg.splits ? src[int64_t(s0 + j) * outs * kBwdOwn * D / 4 + i * 64] : f32x4{};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] += v[j][r / 4][r % 4];
+  }
+  const int64_t bh = tile / own;
+  const int r = int(tile % own) * kBwdOwn + block / DB * 32 + (lane & 31);
+  uint16_t* dst = seg.keys ? (out ? p.dv : p.dk) : p.dq;
+  dst += ((bh / p.H) * p.n_rows + seg.row0 + r) * p.g_st + (bh % p.H) * D + block % DB * 32 + 8 * hh;
+  store_block(dst, acc, seg.keys && out ? 1.f : p.scale, r < seg.len);
 }
 
 // -lse / scale and -D of every row; rows that read nothing get -inf and 0.
@@ -519,8 +612,13 @@ void launch(const BwdParams& p, hipStream_t s) {
   hipLaunchKernelGGL(attn_bwd_rows_kernel<D>, dim3((rows * (D / 8) + 255) / 256), dim3(256), 0, s, p);
   const int64_t bh = int64_t(p.B) * p.H;
   constexpr int NB = 2, NW = kBwdOwn / 32 / NB, ST = 3;
-  hipLaunchKernelGGL((attn_bwd_kernel<D, NB, NW, ST>), dim3(bh * p.n_tiles),
+  hipLaunchKernelGGL((attn_bwd_kernel<D, NB, NW, ST>), dim3(bh * p.n_pieces),
                      dim3(64 * NW), 0, s, p);
+  int64_t tiles = 0;
+  for (int i = 0; i < p.n_seg; ++i)
+    if (p.seg[i].splits > 1) tiles += (p.seg[i].len + kBwdOwn - 1) / kBwdOwn * (1 + p.seg[i].keys);
+  if (tiles > 0)  // four blocks of 32 x 32 per work-group
+    hipLaunchKernelGGL(attn_bwd_merge_kernel<D>, dim3(bh * tiles * (kBwdOwn * D / 4096)), dim3(256), 0, s, p);
 }
 
 }  // namespace

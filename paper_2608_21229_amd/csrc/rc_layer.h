@@ -18,9 +18,11 @@ namespace rc {
 // work-group holds are its own, the rows they meet are streamed.
 struct BwdSeg {
   int32_t row0, len;  // own rows
-  int32_t tile0;      // first own tile, over the segments of both kinds in launch order
+  int32_t piece0;     // first piece, over the segments of both kinds in launch order, per (batch, head)
   int32_t r0, nr;     // streamed ranges
   int32_t keys;       // own rows are keys
+  int32_t splits;     // pieces of a tile's streamed rows; > 1: fp32 partials, merged by a second launch
+  int32_t slot0;      // first partial, per (batch, head), in units of one output's 256 x D
 };
 struct BwdRange {
   int32_t start, len;
@@ -43,7 +45,8 @@ struct BwdParams {
   int64_t st, g_st;    // token strides (elements) of Q/K/V and of the gradients; batch stride N times that
   int32_t B, H, n_rows;
   float scale, scale_log2;
-  int32_t n_seg, n_tiles;
+  float* partial;      // [slots B H, 256, D] in accumulator order
+  int32_t n_seg, n_pieces, n_slots;
   BwdSeg seg[2 * RC_MAX_SEGMENTS];
   BwdRange range[2 * kMaxRanges];
 };

@@ -145,18 +145,28 @@ def test_rows_that_read_nothing_and_keys_nobody_reads():
         assert torch.equal(a[:, 40:], b[:, 40:])
 
 
-def test_batch_entries_and_repeats_are_the_same_bits():
+def test_repeats_are_the_same_bits():
     L = rc.Layout(LONG, "perref")
     q, k, v, o, lse, do, dl = _inputs(L, 2, 3, 128, 17, dlse=True)
     both = rc.full_attention_backward(L, q, k, v, o, lse, do, dlse=dl)
     again = rc.full_attention_backward(L, q, k, v, o, lse, do, dlse=dl)
     for a, b in zip(both, again):
         assert torch.equal(a, b)
-    for b in range(2):
-        at = slice(b, b + 1)
-        one = rc.full_attention_backward(L, q[at], k[at], v[at], o[at], lse[at], do[at], dlse=dl[at])
-        for a, c in zip(both, one):
-            assert torch.equal(a[at], c)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("segs,preset,H", [([(2, 1000)], "dense", 1), ([(0, 37), (1, 130), (2, 1700), (3, 1512), (3, 301)], "paper", 1),
+                                           ([(0, 64), (1, 33), (2, 2500), (3, 700)], "perref", 2),
+                                           ([(0, 300), (1, 1), (2, 3000), (3, 65), (3, 1)], "isolated", 1)])
+def test_few_heads_split_the_streamed_rows(segs, preset, H, D):
+    """Few work-groups: their streamed rows are cut into pieces, whose fp32 sums are merged."""
+    L = rc.Layout(segs, preset)
+    N = sum(n for _, n in segs)
+    assert L.backward_workspace_bytes(1, H, D) > 2 * (H * N * 4 + 16), "no pieces"
+    (q, k, v, o, lse, do, dl), got = _check(L, 1, H, D, seed=37, fused=True, dlse=True)
+    ws = torch.full((L.backward_workspace_bytes(1, H, D) // 4 + 1,), float("nan"), device=DEV)
+    for a, b in zip(rc.full_attention_backward(L, q, k, v, o, lse, do, dlse=dl, workspace=ws), got):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("D", [64, 128])
