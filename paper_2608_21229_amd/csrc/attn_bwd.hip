@@ -365,7 +365,8 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
             const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const float x = dp[nb][8 * ks + r + i];
+              float x = dp[nb][8 * ks + r + i];
+              asm volatile("" : "+v"(x));  // not before this slot
               df[nb][ks][r + i] = (__bf16)(s[nb][8 * ks + r + i] * (KV ? x : x + cd[nb]));
             }
             asm volatile("" : "+v"(df[nb][ks]));
@@ -386,6 +387,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           dp[nb] = mm(fr[g % R], f2[nb][c], dp[nb]);
+          fence();
           if (!KV && nb == 0 && g + PF == DC) next_tile();  // before the first read of S(i + 1)'s rows
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           units(kE1, kE2, 2 * c + nb, 2 * DC);
@@ -402,6 +404,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             am(fr[g % R], pf[nb][f / DB], acc2[nb][f % DB]);
+            fence();
             if (nb == 0) fr[(g + PF) % R] = read(g + PF);
             if (f < DB) units(kE2, 32, 2 * f + nb, 2 * DB);
             else ds(0, 8, 2 * (f - DB) + nb, 2 * DB);
@@ -419,6 +422,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           s2[nb] = mm(fr[g % R], f1[nb][c], s2[nb]);
+          fence();
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV) ds(8, 16, 2 * c + nb, DC);
           else ds(0, 16, 2 * c + nb - 2, 2 * DC - 2);
@@ -441,6 +445,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           am(fr[g % R], df[nb][f / DB], acc1[nb][f % DB]);
+          fence();
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV && f == 2 * DB - 2 && nb == 0) nd = rows16(sn, sthere + 256);
           if (f == 0 && nb == 1) make_arg(0);

@@ -362,39 +362,46 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
 // batch entry and group; the last y: the weights, over all of them.
 __global__ __launch_bounds__(1024) void norm_shared_kernel(const NormParams p) {
   __shared__ float part[16][3][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool in = c < p.C;
   const auto bf = [&](const uint16_t* v, int64_t at) { return __uint_as_float(uint32_t(v[at]) << 16); };
   const int one = int(blockIdx.y), all = p.B * p.G;
   float sum[3] = {0.f, 0.f, 0.f};
-  for (int b = one < all ? one / p.G : 0; b < (one < all ? one / p.G + 1 : p.B) && in; ++b)
-    for (int s = 0; s < p.n_spans; ++s) {
-      const int g = p.span_group[s];
-      if (one < all && g != one % p.G) continue;
-      const int end = s + 1 < p.n_spans ? p.span_chunk0[s + 1] : p.chunks;
+  // a 16th of the flat list (batch entry, chunk) of a batch entry, or of all, in
+  // runs inside one span, eight chunks' loads in flight
+  const int first = one < all ? one / p.G * p.chunks : 0, n = one < all ? p.chunks : p.B * p.chunks;
+  const int last = first + int(int64_t(n) * (wave + 1) / 16);
+  for (int k = first + int(int64_t(n) * wave / 16); k < last;) {
+    const int b = k / p.chunks, chunk = k - b * p.chunks;
+    int s = 0;
+    while (s + 1 < p.n_spans && p.span_chunk0[s + 1] <= chunk) ++s;
+    const int g = p.span_group[s];
+    const int stop = min(last, b * p.chunks + (s + 1 < p.n_spans ? p.span_chunk0[s + 1] : p.chunks));
+    if (in && (one == all || g == one % p.G)) {
       float a[3] = {0.f, 0.f, 0.f};
-      const float* q = p.partial + int64_t(b) * p.chunks * 3 * p.C + c;
-      for (int k0 = p.span_chunk0[s] + wave; k0 < end; k0 += 64) {
-        float v[4][3];
+      const float* q = p.partial + int64_t(k) * 3 * p.C + c;
+      for (int m = stop - k; m > 0; m -= 8, q += int64_t(8) * 3 * p.C) {
+        float v[8][3];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int k = k0 + 16 * j;
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < 3; ++i) v[j][i] = k < end ? q[(int64_t(k) * 3 + i) * p.C] : 0.f;
-        }
+          for (int i = 0; i < 3; ++i) v[j][i] = j < m ? q[int64_t(j * 3 + i) * p.C] : 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
           for (int i = 0; i < 3; ++i) a[i] += v[j][i];
       }
-      const int64_t mod = b * p.mod_sb + int64_t(g) * p.mod_sg + c;
       if (one == all) {
+        const int64_t mod = b * p.mod_sb + int64_t(g) * p.mod_sg + c;
         if (p.scale) a[1] *= 1.f + bf(p.scale, mod);
         if (p.gate) a[2] *= bf(p.gate, mod);
       }
 #pragma unroll
       for (int i = 0; i < 3; ++i) sum[i] += a[i];
     }
+    k = stop;
+  }
 #pragma unroll
   for (int i = 0; i < 3; ++i) part[wave][i][lane] = sum[i];
   __syncthreads();
