@@ -20,4 +20,4 @@ from .binding import (  # noqa: F401
     ROWS_STATIC, ROWS_LIVE, ROWS_CACHED, ROWS_ALL, SPLITS_BALANCED, SPLITS_TAIL, SPLITS_LAST_ROUND,
     RC_OK, RC_ERR_ARG, RC_ERR_UNSUPPORTED, RC_ERR_MASK_NOT_CACHEABLE, RC_ERR_WORKSPACE, RC_ERR_HIP,
 )
-from .chain import Chain  # noqa: F401,E402
+from .chain import Chain, ChainGrads  # noqa: F401,E402
