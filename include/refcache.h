@@ -299,7 +299,8 @@ size_t rc_full_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t
  * Rows that read nothing (lse = -inf) get dq = 0 and add to no key, whatever
  * their o, d_o and dlse hold; keys that nobody reads get dk = dv = 0.
  * Deterministic: the sums keep one order.  RC_ERR_WORKSPACE for a missing or small workspace;
- * RC_ERR_UNSUPPORTED where the mask needs too many merged ranges from either side. */
+ * RC_ERR_UNSUPPORTED where the mask needs too many merged ranges from either side, and for a
+ * scale below 2^-96. */
 rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, int32_t D, float scale,
                                      const void* q, const void* k, const void* v, int64_t tok_stride,
                                      const void* o, const float* lse, const void* d_o, const float* dlse,
@@ -307,7 +308,8 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
                                      void* workspace, size_t ws_bytes, void* stream);
 
 /* Bytes of workspace rc_full_attention_backward needs: two floats per (batch,
- * head, row).  0 on invalid input. */
+ * head, row), and fp32 partials where few heads split their sums.  0 on
+ * invalid input. */
 size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D);
 
 /* FP8 reference cache (the paper calls caching complementary to other
@@ -447,6 +449,7 @@ rc_status rc_gated_norm(const rc_norm* d, const void* h, int64_t ldh, const void
  *   dgate, dscale, dshift  [B, n_groups, C] fp32 out, contiguous; dweight, dpost_weight [C] fp32
  *                 out; each may be NULL.  Groups without rows get zeros.
  *   workspace     rc_gated_norm_backward_workspace_bytes bytes, 16-byte aligned
+ * B * n_groups < 65535 (RC_ERR_UNSUPPORTED).
  * Deterministic: the sums over rows keep one order. */
 rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy, const void* dh, int64_t lddh,
                                  const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,

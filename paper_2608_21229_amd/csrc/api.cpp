@@ -557,6 +557,9 @@ rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
   return RC_OK;
 }
 
+// lse / scale is a first addend of the recomputed scores and has to stay finite.
+constexpr float kBwdMinScale = 0x1p-96f;
+
 size_t bwd_partial_bytes(const BwdParams& p, int64_t bh, int32_t D) {
   return size_t(bh) * p.n_slots * kBwdOwn * D * sizeof(float);
 }
@@ -705,13 +708,17 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   // rows per chunk such that all of them fit one round (every span ends with a
   // shorter one), a multiple of the four rows a work-group takes together.
   const int64_t rows = d->N * d->B;
+  // Where entries and spans alone are more, a span is one chunk.
   int64_t per = std::max<int64_t>(8, (rows + kCUs - 1) / kCUs + 3) / 4 * 4;
-  for (;; per += 4) {
-    int64_t n_chunks = 0;
-    for (int s = 0; s < p.n_spans; ++s) n_chunks += (p.span_rows[s] + per - 1) / per;
-    if (n_chunks * d->B <= kCUs || per >= rows) break;
+  for (;; per += std::max<int64_t>(4, per / 64 / 4 * 4)) {
+    int64_t n_chunks = 0, longest = 0;
+    for (int s = 0; s < p.n_spans; ++s) {
+      n_chunks += (p.span_rows[s] + per - 1) / per;
+      longest = std::max<int64_t>(longest, p.span_rows[s]);
+    }
+    if (n_chunks * d->B <= kCUs || per >= longest) break;
   }
-  p.chunk_rows = int32_t(per);
+  p.chunk_rows = int32_t(std::min<int64_t>(per, INT32_MAX));
   for (int s = 0; s < p.n_spans; ++s) {
     p.span_chunk0[s] = p.chunks;
     p.chunks += (p.span_rows[s] + p.chunk_rows - 1) / p.chunk_rows;
@@ -1013,6 +1020,10 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
                                      void* dv, int64_t grad_stride, void* workspace, size_t ws_bytes, void* stream) {
   RC_TRY(check_layout(L, RC_ENTRY_FULL));
   RC_TRY(check_dims(B, H, D, scale));
+  if (scale < kBwdMinScale) {
+    set_error("softmax scale %g: the attention gradient takes 2^-96 and more", (double)scale);
+    return RC_ERR_UNSUPPORTED;
+  }
   RC_TRY(check_stride(tok_stride, H, D));
   RC_TRY(check_stride(grad_stride, H, D));
   RC_TRY(check_stride(int64_t(H) * D, H, D));  // O and dO
@@ -1304,6 +1315,10 @@ rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy,
   RC_TRY(check_vec(scale, "scale"));
   RC_TRY(check_vec(weight, "weight"));
   RC_TRY(check_vec(post_weight, "post_weight"));
+  if (int64_t(p.B) * p.G >= 65535) {  // a work-group per vector of 64 columns, in the grid's second axis
+    set_error("gated norm: the gradients of B * n_groups = %lld vectors (at most 65534)", (long long)p.B * p.G);
+    return RC_ERR_UNSUPPORTED;
+  }
   const struct {
     const float* p;
     const char* name;

@@ -195,12 +195,12 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
   const bool dy_ = p.dy.p != nullptr, dh_ = p.dh.p != nullptr, x_ = p.x.p != nullptr;
   bf16x8 ry[GP], rn[GP], rh[GP], rx[GP];  // the rows of the next step
   const auto load_rows = [&](int i0) {
-    const int64_t r = row0 + min(i0 + rb, count - 1);
+    const int64_t r = row0 + i0 + rb;
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
       const int c = (t + i * T) * 8;
       ry[i] = rn[i] = rh[i] = rx[i] = bf16x8{};
-      if (!has[i]) continue;
+      if (!has[i] || i0 + rb >= count) continue;  // rows past the chunk are zeros and add nothing
       if (dy_) {
         rn[i] = load8(p.h.p + r * p.h.ld + c);
         ry[i] = load8(p.dy.p + r * p.dy.ld + c);
@@ -276,16 +276,15 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
-      const float rs = rsqrtf(k[0] * p.inv_c + p.eps);
+      const float rs = in ? rsqrtf(k[0] * p.inv_c + p.eps) : 0.f;
       const float mean = p.rms ? 0.f : k[1] * p.inv_c, dot = k[2] * p.inv_c * rs * rs;
-      const float on = in ? 1.f : 0.f, rin = in ? rs : 0.f;
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
         const float* w = vec + (has[i] ? (t + i * T) * 8 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          a_shift[i][e] += d[i][e] * on;
-          a_scale[i][e] += d[i][e] * (n[i][e] * rin);
+          a_shift[i][e] += d[i][e];
+          a_scale[i][e] += d[i][e] * (n[i][e] * rs);
           dh[i][e] += rs * (d[i][e] * w[e] - mean - n[i][e] * dot);
         }
       }
@@ -309,10 +308,10 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
-      rq = rsqrtf(k[0] * p.inv_c + p.eps);
+      rq = in ? rsqrtf(k[0] * p.inv_c + p.eps) : 0.f;
       dot = k[1] * p.inv_c * rq * rq;
     }
-    const float gin = in ? rq * p.rscale : 0.f;
+    const float gq = rq * p.rscale;
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
       const float* w = vec + p.C + (has[i] ? (t + i * T) * 8 : 0);
@@ -320,7 +319,7 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = float(cx[i][e]);
-        a_gate[i][e] += dh[i][e] * (x * gin);
+        a_gate[i][e] += dh[i][e] * (x * gq);
         o[e] = rq * (dh[i][e] * w[e] - x * dot);
       }
       if (in && has[i]) store8(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);

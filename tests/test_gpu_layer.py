@@ -396,6 +396,22 @@ def test_norm_gradient_of_spans(spans):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("C", [64, 1024, 4096])
+def test_norm_gradient_of_idle_row_groups(C):
+    """The last rows of a chunk leave row groups idle: they add nothing, with
+    eps = 0, and in place where a row's gradient overflows bf16."""
+    for N in (1, 9, 13, 70):
+        c = _norm_case(1, [(N, 0)], C, seed=N, post=True)
+        _check_norm_backward(c, "rms", seed=N, post_norm=True, eps=0.0)
+    h, dy = torch.ones(1, 9, C, dtype=BF16, device="cuda"), torch.zeros(1, 9, C, dtype=BF16, device="cuda")
+    h[:, 8, 0] = 2.0
+    dy[:, 8, 1] = 2.0 ** 127
+    shift = torch.zeros(1, 1, C, dtype=BF16, device="cuda")
+    g = rc.gated_norm_backward(dy, h * 2.0 ** -20, shift=shift, norm="rms", eps=0.0, dh_out=dy)
+    assert g.h is dy and bool(torch.isinf(dy[0, 8, 1])) and float(dy[:, :8].abs().max()) == 0.0
+    assert float(g.shift[0, 0, 1]) == 2.0 ** 127 and float(g.shift.abs().sum()) == 2.0 ** 127
+
+
 def test_norm_gradient_against_differences():
     c = _norm_case(1, [(3, 0), (2, 1)], 64, seed=41, weight=True, post=True)
     dy, dh = draw(c["h"].shape, 41, 11), draw(c["h"].shape, 41, 12)

@@ -4,6 +4,7 @@ tables that rc_rotary_init fills.  Pointers are fake and never dereferenced:
 every call below fails validation or has nothing to do."""
 import ctypes
 import math
+import time
 
 import pytest
 import torch
@@ -35,6 +36,7 @@ def bwd(L, B=1, H=2, D=128, scale=0.1, q=FAKE, k=FAKE, v=FAKE, ts=None, o=FAKE, 
     (dict(lse=FAKE + 2), "ARG"), (dict(dlse=FAKE + 1), "ARG"), (dict(dq=None), "ARG"), (dict(dk=None), "ARG"),
     (dict(dv=FAKE + 4), "ARG"), (dict(ts=255), "ARG"), (dict(ts=260), "ARG"), (dict(ts=(1 << 24) + 8), "ARG"),
     (dict(gs=255), "ARG"), (dict(gs=257), "ARG"), (dict(gs=(1 << 24) + 8), "ARG"),
+    (dict(scale=2.0 ** -97), "UNSUPPORTED"), (dict(scale=2.0 ** -96), "WORKSPACE"),
     (dict(), "WORKSPACE"), (dict(ws=None, wsb=1 << 40), "WORKSPACE"), (dict(ws=FAKE + 4, wsb=1 << 40), "WORKSPACE")],
     ids=lambda x: "-".join(f"{k}" for k in x) if isinstance(x, dict) else x)
 def test_gradient_refusals(bad, status):
@@ -199,6 +201,25 @@ def norm_bwd(d, dy=FAKE, lddy=64, dh=FAKE, lddh=64, h=FAKE, ldh=64, x=FAKE, ldx=
     ids=lambda x: "-".join(f"{k}" for k in x) if isinstance(x, dict) else x)
 def test_norm_gradient_refusals(bad, status):
     assert norm_bwd(desc(), **bad) == getattr(rc, "RC_ERR_" + status), message()
+
+
+def test_norm_gradient_of_too_many_vectors():
+    d = desc(B=2, G=32768)
+    assert norm_bwd(d, wsb=1 << 40) == rc.RC_ERR_UNSUPPORTED and "65536" in message()
+    d = desc(B=65535, G=65535)
+    assert norm_bwd(d, wsb=1 << 40) == rc.RC_ERR_UNSUPPORTED
+    assert norm_bwd(desc(B=2, G=32767), wsb=0) == rc.RC_ERR_WORKSPACE
+
+
+def test_norm_chunks_of_many_entries_are_found_at_once():
+    """More entries and spans than CUs: one chunk per span, without a search over every row count."""
+    t0 = time.perf_counter()
+    for B, spans in ((512, ((4000, 0),)), (60_000, ((1, 0), (30_000, 1))), (9, ((1, 0),) * 31 + ((200_000_000, 1),)),
+                     (129, ((1, 0), (8_000_000, 1)))):
+        d = desc(B=B, C=64, N=sum(n for n, _ in spans), spans=spans)
+        need = rc.lib().rc_gated_norm_backward_workspace_bytes(ctypes.byref(d))
+        assert need == B * len(spans) * 3 * 64 * 4
+    assert time.perf_counter() - t0 < 0.5
 
 
 def test_norm_workspace_is_one_round_of_chunks():
