@@ -264,7 +264,19 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
     return l;
   };
   f32x16 s[NB], dp[NB];
-  f32x16 nl, nd;  // dK, dV: the rows' -lse/scale and -D, the products' first addends, read ahead
+  f32x16 nl{}, nd{};  // dK, dV: the rows' -lse/scale and -D, the products' first addends, read ahead
+  // dQ: a lane's -D is one value.  At D = 64 there are registers for it as dP's first addend,
+  // at D = 128 it is added.
+  constexpr bool kAdd = !KV && D == 128;
+  f32x16 od[KV || kAdd ? 1 : NB];
+  if constexpr (!KV && !kAdd) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) od[nb][r] = cd[nb];
+      asm volatile("" : "+v"(od[nb]));
+    }
+  }
   const auto start = [](f32x16 (&x)[NB], const f32x16& c) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -276,17 +288,25 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   };
   // Score e = 0 .. 31 of the lane: the accumulators' first halves of both
-  // blocks, then the second ones.  The argument of a score is computed one
-  // slot before its exponential.
-  float arg = 0.f;
+  // blocks, then the second ones.  The argument of a score is computed kAhead
+  // scores before its exponential.  (An empty statement that pins a value to
+  // its place counts as its producer: the compiler puts a wait state between it
+  // and a use right behind it.)
+  constexpr int kAhead = D == 64 ? 2 : 1;
+  float arg[kAhead];
   const auto make_arg = [&](int e) {
     const float x = s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)];
-    arg = KV ? x * p.scale_log2 : __builtin_fmaf(x, p.scale_log2, cs[(e >> 3) & 1]);
-    asm volatile("" : "+v"(arg));
+    float& a = arg[e % kAhead];
+    a = KV ? x * p.scale_log2 : __builtin_fmaf(x, p.scale_log2, cs[(e >> 3) & 1]);
+    asm volatile("" : "+v"(a));
+  };
+  const auto first_args = [&] {
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) make_arg(e);
   };
   const auto unit = [&](int e) {
-    float t = __builtin_amdgcn_exp2f(arg);
-    if (e < 31) make_arg(e + 1);
+    float t = __builtin_amdgcn_exp2f(arg[e % kAhead]);
+    if (e + kAhead < 32) make_arg(e + kAhead);
     asm volatile("" : "+v"(t));  // stays in its slot
     s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)] = t;
   };
@@ -327,7 +347,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
       for (int nb = 0; nb < NB; ++nb) s[nb] = mm(a, f1[nb][c], s[nb]);
     }
     mask(valid[0]);
-    make_arg(0);
+    first_args();
 #pragma unroll
     for (int e = 0; e < kE1; ++e) unit(e);
 #pragma unroll
@@ -358,18 +378,33 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
         for (int r = 0; r < 8; ++r) pf[nb][ks][r] = (__bf16)s[nb][8 * ks + r];
         asm volatile("" : "+v"(pf[nb][ks]));
       };
-      const auto ds = [&](int from, int to, int slot, int slots) {  // pairs of ds = p dP
+      // Pairs of ds = p dP.  A pair's dP is pinned kAhead pairs before its use, so that it
+      // is not computed in an earlier slot and other instructions lie in between.
+      float dx[kAhead][2];
+      const auto pin_pair = [&](int e) {
+        const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          dx[e % kAhead][i] = dp[nb][8 * ks + r + i];
+          asm volatile("" : "+v"(dx[e % kAhead][i]));
+        }
+      };
+      const auto first_pairs = [&] {
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) pin_pair(e);
+      };
+      const auto ds = [&](int from, int to, int slot, int slots) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (e >= from && e < to && (e - from) * slots / (to - from) == slot) {
             const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float x = dp[nb][8 * ks + r + i];
-              asm volatile("" : "+v"(x));  // not before this slot
-              df[nb][ks][r + i] = (__bf16)(s[nb][8 * ks + r + i] * (KV ? x : x + cd[nb]));
+              const float x = dx[e % kAhead][i];
+              df[nb][ks][r + i] = (__bf16)(s[nb][8 * ks + r + i] * (kAdd ? x + cd[nb] : x));
             }
             asm volatile("" : "+v"(df[nb][ks]));
+            if (e + kAhead < 16) pin_pair(e + kAhead);
           }
       };
       const auto next_tile = [&] {  // the next tile has landed everywhere, its stage's last readers are done
@@ -378,7 +413,10 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
         __builtin_amdgcn_s_barrier();
         start_tile();
       };
-      start(dp, nd);
+      if constexpr (KV || kAdd) start(dp, nd);
+      else
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) dp[nb] = od[nb];
       fence();
       int g = 0;
       // dP(i)
@@ -409,6 +447,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
             if (f < DB) units(kE2, 32, 2 * f + nb, 2 * DB);
             else ds(0, 8, 2 * (f - DB) + nb, 2 * DB);
             if (f == DB - 1) pack(1, nb);
+            if (f == DB - 1 && nb == 1) first_pairs();
             if (f == 2 * DB - 1 && nb == 0) nl = rows16(sn, sthere);
             fence();
           }
@@ -426,7 +465,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV) ds(8, 16, 2 * c + nb, DC);
           else ds(0, 16, 2 * c + nb - 2, 2 * DC - 2);
-          
+          if (!KV && c == 0 && nb == 1) first_pairs();
           fence();
         }
       }
@@ -448,7 +487,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           fence();
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV && f == 2 * DB - 2 && nb == 0) nd = rows16(sn, sthere + 256);
-          if (f == 0 && nb == 1) make_arg(0);
+          if (f == 0 && nb == 1) first_args();
           units(0, kE1, 2 * f + nb - 2, 4 * DB - 2);
           if (j == 1)
 #pragma unroll
