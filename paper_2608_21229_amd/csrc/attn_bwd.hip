@@ -4,6 +4,40 @@
 // sum_d dO_id O_id - dlse_i:
 //   ds_ij = p_ij (dO_i v_j - D_i)
 //   dq_i = scale sum_j ds_ij k_j   dk_j = scale sum_i ds_ij q_i   dv_j = sum_i p_ij dO_i
+//
+// Five products per pair (S = QK, dP = dO V, dV, dK, dQ).  dV and dK sum over
+// queries, dQ over keys, so one pass over the pairs would have to add one of
+// them to memory from many work-groups: in an order that changes the sums, or
+// through one fp32 partial of dQ per 256 keys (two 1024-pixel samples of 24
+// heads: 7 GB written and read, 3 ms).  Two kinds of work-groups in one launch
+// compute seven products instead and write every output once: those that hold
+// 256 keys stream the queries that see them (S, dP, dV, dK), those that hold 256
+// queries stream the keys they see (S, dP, dQ).
+//
+// Layout of the work.  A wave holds 64 own rows as two blocks of 32 (operands in
+// registers, sums in accumulation registers), so that a fragment read from LDS
+// feeds two products (one block and eight waves: 817 us for the ragged D = 64
+// case against 644).  Four waves share a 3-stage ring of 64 streamed rows of two
+// tensors, loaded straight to LDS (4 to 6 stages measured the same).  One wave
+// per SIMD, so nothing but its own order hides latency: the loop is one stream of
+// slots, each a product followed by its share of the other work (a fragment read
+// PF products ahead, one or two exponentials, a pair of ds, a load of the next
+// stage), and fences keep the compiler from moving work between slots.  The
+// scores of the next 32 rows are computed before dK (dQ) of the present ones, so
+// that their exponentials have products to hide behind.
+//
+// Rounding: P and ds are rounded to bf16 (off by at most 2^-8 of each) as operands
+// of the products dV, dK and dQ; scores, exponentials, dP and all sums stay fp32.
+// The statistics enter in fp32: keys start S from -lse / scale and dP from -D (a
+// row's value is the accumulator's first addend), queries subtract them.
+//
+// What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.70 ms, 955 TFLOP/s
+// of five products, 1340 of the seven computed, which is what a large library
+// matrix product reaches here; the matrix pipes are busy 61% of the time at a
+// clock that falls under the load.  With exponentials, ds, fragment reads and loads
+// taken out the same products take 2.83 ms; the loads alone are 2%, the reads 3%.
+// D = 64 has half the products per exponential and is bound by issue: 613 us for the
+// ragged case, 501 without exponentials and ds.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -56,6 +90,8 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return int64_t(uint64_t(hi) << 32 | lo);
 }
 
+// D: head width; KV: own rows are keys; NB blocks of 32 own rows per wave; NW
+// waves; ST stages.
 template <int D, bool KV, int NB, int NW, int ST>
 struct Bwd {
   static constexpr int GR = D / 8, DC = D / 16, DB = D / 32;
@@ -93,10 +129,19 @@ __device__ __forceinline__ void store_block(uint16_t* out, const f32x16& acc, fl
   }
 }
 
+// One piece of an own tile: its share of the streamed rows, and the stores.
+//
+// The accumulator products are single statements of assembly ("+a"): the
+// compiler would move the sums of 16 registers between files around every
+// product.  It does not see their hazards: two wait states lie between a vector
+// instruction and a product that reads its result (a read, a fence's slot), and
+// `settle` waits for the last ones; both are checked in the built assembly by a
+// test.
 template <int D, bool KV, int NB, int NW, int ST>
 __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const BwdSeg seg, int bh, int t, int piece) {
   using T = Bwd<D, KV, NB, NW, ST>;
-  constexpr int PF = D == 64 ? 3 : 2;  // fragments read ahead of their MFMAs
+  // fragments read ahead of their MFMAs (D = 128 has no registers for a third)
+  constexpr int PF = D == 64 ? 3 : 2;
   constexpr int GR = T::GR, DC = T::DC, DB = T::DB, kT = T::kT;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -265,8 +310,8 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   };
   f32x16 s[NB], dp[NB];
   f32x16 nl{}, nd{};  // dK, dV: the rows' -lse/scale and -D, the products' first addends, read ahead
-  // dQ: a lane's -D is one value.  At D = 64 there are registers for it as dP's first addend,
-  // at D = 128 it is added.
+  // dQ: a lane's -D is one value.  At D = 64 there are registers for it as dP's first addend
+  // (623 -> 613 us for the ragged case), at D = 128 it is added.
   constexpr bool kAdd = !KV && D == 128;
   f32x16 od[KV || kAdd ? 1 : NB];
   if constexpr (!KV && !kAdd) {
@@ -580,7 +625,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
   else bwd_tile<D, false, NB, NW, ST>(p, ring, seg, bh, t, piece);
 }
 
-// The pieces of split tiles, summed in order.  A wave takes one 32 x 32 block; its
+// The pieces of split tiles, summed in order (fp32), bound by the partials' bytes.
+// With few heads the split pays for it: five references, one head 897 us unsplit,
+// 335 split; a 512-pixel edit, three heads 142 and 64.  A wave takes one 32 x 32 block; its
 // partials' loads are in flight together, four pieces at a time.
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) {
@@ -626,7 +673,8 @@ __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) 
   store_block(dst, acc, seg.keys && out ? 1.f : p.scale, r < seg.len);
 }
 
-// -lse / scale and -D of every row; rows that read nothing get -inf and 0.
+// -lse / scale and -D of every row; rows that read nothing get -inf and 0.  One
+// pass over o and d_o, 16 bytes a lane: HBM-bound (47 us for the 215 MB of two 1024-pixel samples).
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_rows_kernel(const BwdParams p) {
   constexpr int L = D / 8;

@@ -5,7 +5,12 @@
 // Backward: u is the gradient turned back; with a norm, xh = x r:
 //   dx = r (u w - xh mean(u w xh)),  dw = sum over all rows of u xh
 //
-// HBM-bound: every row is read and written once.  A head row is D / 8 lanes of 16
+// The norm's sums and the rotation are fp32 (angles reduced in 64 bits); each
+// output is rounded once.
+//
+// HBM-bound: every row is read and written once: 4608 tokens of 24 heads, D = 128,
+// with the norm 21 us (113 MB); 2 x 7801 tokens of 12 heads backward 71 us (288 MB,
+// 4.1 TB/s) and 4 us for dw.  A head row is D / 8 lanes of 16
 // bytes, so a wave holds 512 / D head rows; it takes a token's rows of one
 // tensor after another, kAhead loads in flight, with the token's sines and
 // cosines (and the norm's weights) in registers.  out[e] = r (x[e] A[e] + x'[e] B[e])
@@ -156,7 +161,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
 }
 
 // Backward with a norm: a work-group takes a contiguous run of tokens, its
-// waves every fourth of them, and leaves its sums of dw.
+// waves every fourth of them, and leaves its sums of dw.  Three work-groups per CU
+// (their registers' limit): 4608 x 24 and 15602 x 12 head rows take 36.4 and 58.4 us with
+// 768, 42.9 and 80.0 with 256, 47.8 and 69.6 with 1024, whose last 256 run alone.
 template <int D, bool HALVES>
 __global__ __launch_bounds__(256, 3) void rotary_norm_backward_kernel(const RotaryParams p) {
   constexpr int L = D / 8, RW = 64 / L;
