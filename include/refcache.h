@@ -25,6 +25,12 @@
  * (rc_ref_kv_prefill_fp8, rc_step_masked_attention_fp8), and rc_linear is the
  * dense projection of the chained synthetic layer built around them.
  *
+ * For training and for whole layers:
+ *   rc_full_attention_backward  the gradient of the recompute under any mask.
+ *   rc_qk_rotary                RMS norm and rotation of queries and keys by position,
+ *   rc_gated_norm               residual with a gated block output, norm and modulation,
+ *                               each with its gradient (*_backward).
+ *
  * Common conventions
  *   Element type   bf16 for Q, K, V, O and the cache (passed as raw bits;
  *                  the FP8 entries store the cache as e4m3 codes with fp32

@@ -2,7 +2,8 @@
 path of arXiv 2608.21229: block-masked attention over
 [static text anchors | live text | target | references], with a
 once-per-request reference K/V prefill, per-step masked attention over fresh
-plus cached K/V, and a full-recompute baseline.
+plus cached K/V, and a full-recompute baseline; for training, the gradient of
+the recompute, and the norms and rotation around the attention with theirs.
 
 The compute lives in ``librefcache.so`` (hand-written HIP, C ABI declared in
 ``include/refcache.h``); ``binding`` is its ctypes wrapper and ``chain``

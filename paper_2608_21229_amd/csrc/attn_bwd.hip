@@ -31,8 +31,8 @@
 // The statistics enter in fp32: keys start S from -lse / scale and dP from -D (a
 // row's value is the accumulator's first addend), queries subtract them.
 //
-// What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.70 ms, 955 TFLOP/s
-// of five products, 1340 of the seven computed, which is what a large library
+// What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.66 ms, 967 TFLOP/s
+// of five products, 1350 of the seven computed, which is what a large library
 // matrix product reaches here; the matrix pipes are busy 61% of the time at a
 // clock that falls under the load.  With exponentials, ds, fragment reads and loads
 // taken out the same products take 2.83 ms; the loads alone are 2%, the reads 3%.
