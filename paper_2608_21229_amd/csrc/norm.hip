@@ -12,8 +12,8 @@
 // pass over the registers (the row is in them); each output is rounded once.
 //
 // HBM-bound: every row is read once and written once.  4608 rows of 2560 channels
-// forward 17 us (94 MB, partly from cache); 8768 rows backward 63 us (269 MB, 4.3
-// TB/s) and 6.6 us for the gradients shared by the rows.
+// forward 17 us (94 MB, partly from cache); 8768 rows backward 59 us (269 MB, 4.6
+// TB/s) and 6.5 us for the gradients shared by the rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -182,14 +182,19 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 // factors of the column).  The chunk's vectors (1 + scale) w and a gate w_p lie in
 // LDS; the next rows are loaded before the present ones are computed, except
 // with 4 granules a thread, whose registers that would overflow (1280 rows of 16384
-// channels: 144 us, 90 without).
+// channels: 144 us, 90 without).  The vectors' planes keep LDS reads free of bank
+// conflicts (two samples' 3936 rows of 1928 channels: 59.6 -> 52.9 us with the sums).
 template <int T, int GP>
 __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) {
   constexpr int NT = 512;
   constexpr bool kAhead = GP < 4;
   __shared__ RowSums<1> lds1;
   __shared__ RowSums<3> lds3;
-  __shared__ __attribute__((aligned(16))) float vec[2 * T * GP * 8];  // [2, C], at the end the row groups' sums
+  // two vectors (at the end the row groups' sums): the first four channels of all
+  // granules, then the others, so that lanes next to each other read 16 bytes next to each other
+  constexpr int kPlane = T * GP * 4;
+  __shared__ __attribute__((aligned(16))) float vec[4 * kPlane];
+  const auto at_vec = [](int g, int e) { return (e >> 2) * kPlane + g * 4 + (e & 3); };
   constexpr int RB = NT / T;
   const int t = threadIdx.x % T, rb = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
   const int64_t b = blockIdx.x / p.chunks;
@@ -238,7 +243,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     times(a, p.gate ? p.gate + mod : nullptr);
     times(a, p.post_weight);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vec[g * 8 + e] = s[e], vec[p.C + g * 8 + e] = a[e];
+    for (int e = 0; e < 8; ++e) vec[at_vec(g, e)] = s[e], vec[2 * kPlane + at_vec(g, e)] = a[e];
   }
   __syncthreads();
 
@@ -280,10 +285,10 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
       float k[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const float* w = vec + (has[i] ? (t + i * T) * 8 : 0);
+        const float* w = vec + (has[i] ? (t + i * T) * 4 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float dn = d[i][e] * w[e];
+          const float dn = d[i][e] * w[at_vec(0, e)];
           k[0] += n[i][e] * n[i][e];
           k[1] += dn;
           k[2] += dn * n[i][e];
@@ -294,12 +299,12 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
       const float mean = p.rms ? 0.f : k[1] * p.inv_c, dot = k[2] * p.inv_c * rs * rs;
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const float* w = vec + (has[i] ? (t + i * T) * 8 : 0);
+        const float* w = vec + (has[i] ? (t + i * T) * 4 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           a_shift[i][e] += d[i][e];
           a_scale[i][e] += d[i][e] * (n[i][e] * rs);
-          dh[i][e] += rs * (d[i][e] * w[e] - mean - n[i][e] * dot);
+          dh[i][e] += rs * (d[i][e] * w[at_vec(0, e)] - mean - n[i][e] * dot);
         }
       }
     }
@@ -313,12 +318,12 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     if (p.post) {
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const float* w = vec + p.C + (has[i] ? (t + i * T) * 8 : 0);
+        const float* w = vec + 2 * kPlane + (has[i] ? (t + i * T) * 4 : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float x = float(cx[i][e]);
           k[0] += x * x;
-          k[1] += dh[i][e] * w[e] * x;
+          k[1] += dh[i][e] * w[at_vec(0, e)] * x;
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
@@ -328,13 +333,13 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     const float gq = rq * p.rscale;
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
-      const float* w = vec + p.C + (has[i] ? (t + i * T) * 8 : 0);
+      const float* w = vec + 2 * kPlane + (has[i] ? (t + i * T) * 4 : 0);
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = float(cx[i][e]);
         a_gate[i][e] += dh[i][e] * (x * gq);
-        o[e] = rq * (dh[i][e] * w[e] - x * dot);
+        o[e] = rq * (dh[i][e] * w[at_vec(0, e)] - x * dot);
       }
       if (in && has[i]) store8(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
     }
@@ -351,14 +356,14 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
 #pragma unroll
           for (int i = 0; i < GP; ++i) {
             if (!has[i]) continue;
-            float* at = vec + (t + i * T) * 8;
+            float* at = vec + (t + i * T) * 4;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) at[e] = w == 0 ? a[i][e] : at[e] + a[i][e];
+            for (int e = 0; e < 8; ++e) at[at_vec(0, e)] = w == 0 ? a[i][e] : at[at_vec(0, e)] + a[i][e];
           }
         }
       }
       __syncthreads();
-      for (int c = threadIdx.x; c < p.C; c += NT) out[q * p.C + c] = vec[c];
+      for (int c = threadIdx.x; c < p.C; c += NT) out[q * p.C + c] = vec[at_vec(c / 8, c % 8)];
     } else {
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
@@ -458,9 +463,9 @@ void launch_bwd(const NormParams& p, hipStream_t s) {
 //   forward    28.8    27.4    29.1    28.6    36.1
 //              33.1    28.6    28.4    26.7    27.9
 //              45.5    32.3    28.4    27.8    27.4
-//   backward   54.3    55.8    60.5    77.0       -
-//              85.0    64.2    58.8    64.5   107.5
-//             142.4    88.9    59.6    69.3    58.0
+//   backward   53.9    54.9    59.0   128.1       -
+//              82.3    60.4    57.2    61.5    60.4
+//             141.2    88.5    58.5    66.8    55.2
 int launch_norm(const NormParams& p, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int ng = p.C / 8;
