@@ -33,9 +33,9 @@
 //
 // What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.66 ms, 967 TFLOP/s
 // of five products, 1350 of the seven computed, which is what a large library
-// matrix product reaches here; the matrix pipes are busy 61% of the time at a
-// clock that falls under the load.  With exponentials, ds, fragment reads and loads
-// taken out the same products take 2.83 ms; the loads alone are 2%, the reads 3%.
+// matrix product reaches here; the matrix pipes are busy 71% of the cycles and the
+// clock falls to 1.7 GHz.  With exponentials, ds, fragment reads and loads taken out
+// the same products take 2.83 ms; the loads alone are 2%, the reads 3%.
 // D = 64 has half the products per exponential and is bound by issue: 613 us for the
 // ragged case, 501 without exponentials and ds.
 #include <hip/hip_runtime.h>
