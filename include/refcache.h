@@ -397,7 +397,8 @@ rc_status rc_rotary_init(rc_rotary* R, int32_t head_dim, int32_t n_axes, const i
  *   q_norm, k_norm  [D] bf16, NULL: no norm
  *   q_out, k_out  as q and k, token stride out_stride; each may be its input (same
  *                 stride), otherwise they overlap nothing
- * B * N < 2^31.  N = 0 is a no-op.  RC_ERR_UNSUPPORTED for head_dim other than 64/128. */
+ * B * N < 2^31, and fewer than 2^32 threads (64 per token and 48 head rows of 128, 96 of 64;
+ * RC_ERR_ARG).  N = 0 is a no-op.  RC_ERR_UNSUPPORTED for head_dim other than 64/128. */
 rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* q, const void* k,
                        int64_t tok_stride, const void* positions, int32_t pos_float, int32_t pos_batch,
                        const void* q_norm, const void* k_norm, float eps, void* q_out, void* k_out,
@@ -442,7 +443,8 @@ typedef struct {
  *   gate, scale, shift, weight [C], post_weight [C]  bf16, each may be NULL (ones; shift: zeros)
  *   h_out         h' rounded; may be h (same stride).  y is computed from h' before its rounding
  *   y             NULL: only the residual
- * Outputs overlap no input except as said.  N = 0 is a no-op. */
+ * Outputs overlap no input except as said.  N = 0 is a no-op.  A launch has fewer than
+ * 2^32 threads: B * N < 2^26 with C <= 1024, < 2^24 with more (RC_ERR_ARG). */
 rc_status rc_gated_norm(const rc_norm* d, const void* h, int64_t ldh, const void* x, int64_t ldx, const void* gate,
                         const void* scale, const void* shift, const void* weight, const void* post_weight,
                         void* h_out, int64_t ldho, void* y, int64_t ldy, void* stream);

@@ -84,6 +84,9 @@ class Chain:
         if positions is not None:
             for which in (rcb.ROWS_STATIC, rcb.ROWS_LIVE):
                 self._positions[which] = self._rows_of(positions, which)
+            # gathered on the stream that is current here, read on every call's
+            if positions.is_cuda:
+                rcb._torch().cuda.current_stream(positions.device).synchronize()
 
     def _rows_of(self, t, which: int):
         """The rows of a class out of a tensor over all tokens."""
@@ -159,7 +162,10 @@ class Chain:
         if self.rotary is None:
             return q, k
         q_norm, k_norm = self._norms(l)
-        return rcb.qk_rotary(self.rotary, q, k, self._positions[rows_kind], q_norm=q_norm, k_norm=k_norm, eps=self.eps,
+        positions = self._positions[rows_kind]
+        if stream is not None:  # the chain may be dropped while the stream still reads them
+            positions.record_stream(rcb._torch().cuda.current_stream(q.device))
+        return rcb.qk_rotary(self.rotary, q, k, positions, q_norm=q_norm, k_norm=k_norm, eps=self.eps,
                              q_out=q if q_out is None else q_out, k_out=k if k_out is None else k_out, stream=stream)
 
     def _layers(self, h, rows_kind, attend, collect, last_out, stream, modulation):

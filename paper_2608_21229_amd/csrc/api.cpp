@@ -638,6 +638,11 @@ int32_t rotary_groups(const RotaryParams& p, int32_t D) {
   return int32_t(std::max<int64_t>(1, std::min<int64_t>({g, all, 12})));
 }
 
+int64_t rotary_splits(const RotaryParams& p, int32_t D) {  // waves per token
+  const int rw = 512 / D;
+  return (int64_t(p.H + rw - 1) / rw * (p.x[0] && p.x[1] ? 2 : 1) + p.groups - 1) / p.groups;
+}
+
 int32_t rotary_blocks(int32_t B, int64_t N) {
   return int32_t(std::max<int64_t>(1, std::min<int64_t>(kRotaryBlocks, (N * B + 3) / 4)));
 }
@@ -723,6 +728,15 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   for (int s = 0; s < p.n_spans; ++s) {
     p.span_chunk0[s] = p.chunks;
     p.chunks += (p.span_rows[s] + p.chunk_rows - 1) / p.chunk_rows;
+  }
+  return RC_OK;
+}
+
+// A launch's threads are counted in 32 bits.
+rc_status check_threads(int64_t blocks, int64_t threads, const char* what) {
+  if (blocks > ((int64_t(1) << 32) - 1) / threads) {
+    set_error("%s launch of %lld x %lld threads exceeds the grid limit", what, (long long)blocks, (long long)threads);
+    return RC_ERR_ARG;
   }
   return RC_OK;
 }
@@ -1046,8 +1060,8 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   BwdParams p;
   memset(&p, 0, sizeof p);
   RC_TRY(plan_bwd(L, int64_t(B) * H, p));
-  RC_TRY(check_blocks(int64_t(B) * H * p.n_pieces, "attention gradient"));
-  RC_TRY(check_blocks((rows * (D / 8) + 255) / 256, "attention gradient"));
+  RC_TRY(check_threads(int64_t(B) * H * p.n_pieces, 256, "attention gradient"));
+  RC_TRY(check_threads((rows * (D / 8) + 255) / 256, 256, "attention gradient"));
   const size_t need = 2 * bwd_row_bytes(rows) + bwd_partial_bytes(p, int64_t(B) * H, D);
   if (!workspace || !aligned16(workspace) || ws_bytes < need) {
     set_error("the attention gradient needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
@@ -1146,7 +1160,7 @@ rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, cons
   p.y_st = out_stride;
   p.sign = 1.f;
   p.groups = rotary_groups(p, D);
-  RC_TRY(check_blocks(B * N * ((int64_t(H) * D + 511) / 512 * 2), "rotation"));
+  RC_TRY(check_threads((B * N * rotary_splits(p, D) + 3) / 4, 256, "rotation"));
   RC_TRY(check_launcher(launch_rotary, "rotation"));
   RC_TRY(hip_status(launch_rotary(p, D, stream), "rotation launch"));
   return RC_OK;
@@ -1195,10 +1209,10 @@ rc_status rc_qk_rotary_backward(const rc_rotary* R, int32_t B, int64_t N, int32_
   p.n_st = tok_stride;
   p.y_st = out_stride;
   p.sign = -1.f;
-  RC_TRY(check_blocks(B * N * ((int64_t(H) * D + 511) / 512 * 2), "rotation gradient"));
   if (!norm) {
     if (N == 0) return RC_OK;
     p.groups = rotary_groups(p, D);
+    RC_TRY(check_threads((B * N * rotary_splits(p, D) + 3) / 4, 256, "rotation gradient"));
     RC_TRY(check_launcher(launch_rotary, "rotation gradient"));
     RC_TRY(hip_status(launch_rotary(p, D, stream), "rotation gradient launch"));
     return RC_OK;
@@ -1261,6 +1275,7 @@ rc_status rc_gated_norm(const rc_norm* d, const void* h, int64_t ldh, const void
   p.shift = static_cast<const uint16_t*>(shift);
   p.weight = static_cast<const uint16_t*>(weight);
   p.post_weight = static_cast<const uint16_t*>(post_weight);
+  RC_TRY(check_threads(p.N * p.B, p.C <= 1024 ? 64 : 256, "gated norm"));
   RC_TRY(check_launcher(launch_norm, "gated norm"));
   RC_TRY(hip_status(launch_norm(p, stream), "gated norm launch"));
   return RC_OK;

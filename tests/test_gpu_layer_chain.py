@@ -179,3 +179,37 @@ def test_gradient_of_the_chain(B, H, D, mask, modulated, norms, kind):
     again = chain.full_backward(h, dh, modulation=mod, stream=s)
     s.synchronize()
     assert torch.equal(again.h, got.h) and torch.equal(again.w_qkv[0], got.w_qkv[0])
+
+
+def test_chain_captured_and_replayed():
+    """A cached step and the gradient of the recompute, each captured once and
+    replayed with eager work of the same chain in between; two graphs and the
+    eager calls share nothing but inputs."""
+    segs = [(0, 17), (1, 40), (2, 130), (3, 70)]
+    chain, h, mod = make(segs, "perref", 1, 2, 64, 2, seed=9)
+    live, static = rows_of(segs, True), rows_of(segs, False)
+    h_live, h_static, dh = h[:, live].contiguous(), h[:, static].contiguous(), draw(h.shape, 9, 71)
+    m_live, m_static = mod[:, :1].contiguous(), mod[:, 1:].contiguous()
+    flat = lambda g: [g.h, *g.w_qkv, *g.w_o, *g.q_norms, *g.k_norms, g.modulation]  # noqa: E731
+
+    def eager():
+        caches = chain.prefill(h_static, modulation=m_static)
+        return caches, chain.step(h_live, caches, modulation=m_live), chain.full_backward(h, dh, modulation=mod)
+
+    caches, step, grads = eager()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        step_out = chain.step(h_live, caches, modulation=m_live)
+    with torch.cuda.graph(graphs[1]):
+        grads_out = chain.full_backward(h, dh, modulation=mod)
+    for i in range(3):
+        for t in [step_out, *flat(grads_out)]:
+            t.fill_(float("nan"))
+        for g in graphs if i % 2 else reversed(graphs):
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(step_out, step)
+        for a, b in zip(flat(grads_out), flat(grads)):
+            assert torch.equal(a, b)
+        eager()

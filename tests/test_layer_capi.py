@@ -232,6 +232,20 @@ def test_norm_workspace_is_one_round_of_chunks():
             assert chunks == int(chunks) and len(spans) * B <= chunks <= max(256, len(spans) * B)
 
 
+def test_launches_beyond_32_bits_of_threads():
+    """Refused before any HIP call (the calls that fit fail later, at their workspace, or are not made)."""
+    L = rc.Layout([(1, 4), (2, 4)], "dense")
+    assert bwd(L, B=65535, H=65535, D=64) == rc.RC_ERR_ARG and "grid limit" in message()
+    assert bwd(L, B=4096, H=2047, D=64) == rc.RC_ERR_WORKSPACE
+    R = init()[1]
+    assert rot(R, B=1, N=(1 << 26) + 1, H=1) == rc.RC_ERR_ARG and "grid limit" in message()
+    assert rot_bwd(R, B=2, N=(1 << 26), H=1) == rc.RC_ERR_ARG and "grid limit" in message()
+    n = 1 << 24
+    assert norm(desc(B=4, N=n, spans=((n, 0),))) == rc.RC_ERR_ARG and "grid limit" in message()
+    assert norm(desc(B=1, C=2048, N=n, mb=0, mg=0, spans=((n, 0),)), ldh=2048, ldx=2048, ldho=2048, ldy=2048) == rc.RC_ERR_ARG
+    assert "grid limit" in message()
+
+
 # ---------------------------------------------------------------- binding
 def test_binding_takes_gpu_tensors_only():
     L = rc.Layout(SEGS, "perref")
