@@ -474,18 +474,29 @@ rc_layout key_layout(const rc_layout* L) {
   return t;
 }
 
+// Own tiles have 256 rows (64 a wave), or 128, which take two thirds of the time:
+// few rows or heads are done sooner, many cost a third more.  Costs in 0.04 us of
+// a streamed tile ([D = 128][own tile][keys]), of a work-group's other work (own
+// rows, first loads, stores) and of the merge's launch; a partial of 256 x 128,
+// written and read, is 1.  (Splits at 1.5 and a merge at 100: one head of five
+// references 365 us, 323 with these.)
+constexpr int kBwdOwn[2] = {256, 128};
+constexpr int kBwdTile[2][2][2] = {{{34, 36}, {20, 22}}, {{50, 56}, {34, 38}}};
+constexpr int kBwdFixed[2][2] = {{80, 60}, {110, 80}};
+constexpr int kBwdMerge = 70;
+
 // The schedule of the attention gradient for bh (batch, head)s, from the plans of
 // full recomputes of the layout and of its keys.
-rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
+rc_status plan_bwd(const rc_layout* L, int64_t bh, int32_t D, BwdParams& b) {
   const rc_layout kl = key_layout(L);
   constexpr int kMax = 2 * RC_MAX_SEGMENTS;
   BwdSeg seg[kMax];
-  int64_t tiles[kMax], count[kMax];  // streamed tiles of an own tile, own tiles over all heads
+  int64_t tiles[kMax];  // streamed tiles of an own tile
   int n = 0;
   for (int keys = 0; keys < 2; ++keys) {
     Params p;
     memset(&p, 0, sizeof p);
-    p.bm = kBwdOwn;
+    p.bm = kBwdOwn[0];
     RC_TRY(plan(keys ? &kl : L, RC_ENTRY_FULL, p));
     const int first = n;
     for (int i = 0; i < kMaxRanges; ++i)
@@ -503,43 +514,46 @@ rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
       seg[n++] = BwdSeg{q.row0, q.len, 0, keys * kMaxRanges + q.r0, q.nr, keys, 1, 0};
     }
   }
-  // Pieces of a tile's streamed rows, so that few heads fill the chip: of at
-  // most `most` tiles each.  Costs in fifths of a tile of queries' time (a tile of
-  // keys takes six); a piece costs two tiles besides (own rows, first loads,
-  // stores); the launch ends with its longest piece, or with the work spread
-  // over the CUs and a part of a piece.  A split costs the merge's launch and the
-  // partials (one of 128 KB, written and read, is 9 hundredths).
+  // The own tile, and pieces of at most `most` of its streamed tiles, so that few
+  // heads fill the chip.  The launch ends with its longest work-group, or with the
+  // work spread over the CUs (where first loads and stores half hide) and a part of
+  // one.  Drawn sizes of 26 to 5100 rows and 1 to 24 heads: 41 us in the geometric mean with
+  // whole 256-row tiles, 34.0 with pieces, 28.9 with 128-row tiles too.
   int64_t longest = 1;
-  for (int i = 0; i < n; ++i) {
-    count[i] = bh * ((seg[i].len + kBwdOwn - 1) / kBwdOwn);
-    longest = std::max(longest, tiles[i]);
-  }
+  for (int i = 0; i < n; ++i) longest = std::max(longest, tiles[i]);
   const auto splits_of = [&](int i, int64_t most) { return std::max<int64_t>(1, (tiles[i] + most - 1) / most); };
-  const auto cost_of = [&](int i, int64_t most) {
+  const auto cost_of = [&](int i, int64_t most, int own) {
     const int64_t s = splits_of(i, most);
-    return ((tiles[i] + s - 1) / s + 2) * (seg[i].keys ? 6 : 5);
+    return (tiles[i] + s - 1) / s * kBwdTile[D == 128][own][seg[i].keys];
   };
   int64_t best = INT64_MAX, best_most = longest;
-  for (int64_t s = 1; s <= 32 && (s == 1 || (longest + s - 1) / s >= 4); ++s) {
-    const int64_t most = (longest + s - 1) / s;
-    int64_t top = 0, total = 0, slots = 0;
-    for (int i = 0; i < n; ++i) {
-      const int64_t k = splits_of(i, most), c = cost_of(i, most);
-      top = std::max(top, c);
-      total += count[i] * k * c;
-      if (k > 1) slots += count[i] * k * (1 + seg[i].keys);
+  int best_own = 0;
+  for (int own = 0; own < 2; ++own) {
+    for (int64_t s = 1; s <= 32 && (s == 1 || (longest + s - 1) / s >= 2); ++s) {
+      const int64_t most = (longest + s - 1) / s;
+      int64_t top = 0, total = 0, slots = 0;
+      for (int i = 0; i < n; ++i) {
+        const int64_t k = splits_of(i, most), c = cost_of(i, most, own);
+        const int64_t count = bh * ((seg[i].len + kBwdOwn[own] - 1) / kBwdOwn[own]);
+        top = std::max(top, c);
+        total += count * k * (c + kBwdFixed[D == 128][own] / 2);
+        if (k > 1) slots += count * k * (1 + seg[i].keys);
+      }
+      top += kBwdFixed[D == 128][own];
+      int64_t est = std::max(top, total / kCUs + top / 3);
+      if (s > 1) est += kBwdMerge + slots * D * kBwdOwn[own] / (256 * 128);
+      const bool plain = best_most == longest && best_own == 0;  // another form has to gain 10%
+      if ((s == 1 && own == 0) || est * 10 < best * (plain ? 9 : 10)) best = est, best_most = most, best_own = own;
     }
-    int64_t est = std::max(top, total / kCUs + top / 3);
-    if (s > 1) est += 10 + slots * 9 / 100;
-    if (s == 1 ? true : est * 10 < best * 9 || (best_most < longest && est < best)) best = est, best_most = most;
   }
+  b.own = kBwdOwn[best_own];
   // Work-groups run in this order: the longest first, so that the launch ends
   // with short ones (in the order of the segments, queries after keys: 512-pixel
   // edit 348 us, longest first 324).
   int order[kMax];
   for (int i = 0; i < n; ++i) order[i] = i;
   std::sort(order, order + n, [&](int x, int y) {
-    const int64_t cx = cost_of(x, best_most), cy = cost_of(y, best_most);
+    const int64_t cx = cost_of(x, best_most, best_own), cy = cost_of(y, best_most, best_own);
     return cx != cy ? cx > cy : x < y;
   });
   b.n_seg = n;
@@ -547,7 +561,7 @@ rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
   for (int i = 0; i < n; ++i) {
     BwdSeg& g = b.seg[i];
     g = seg[order[i]];
-    const int own = (g.len + kBwdOwn - 1) / kBwdOwn;
+    const int own = (g.len + b.own - 1) / b.own;
     g.splits = int32_t(splits_of(order[i], best_most));
     g.piece0 = b.n_pieces;
     b.n_pieces += own * g.splits;
@@ -561,7 +575,7 @@ rc_status plan_bwd(const rc_layout* L, int64_t bh, BwdParams& b) {
 constexpr float kBwdMinScale = 0x1p-96f;
 
 size_t bwd_partial_bytes(const BwdParams& p, int64_t bh, int32_t D) {
-  return size_t(bh) * p.n_slots * kBwdOwn * D * sizeof(float);
+  return size_t(bh) * p.n_slots * p.own * D * sizeof(float);
 }
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
@@ -1025,7 +1039,7 @@ size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H
   if (check_layout(L, RC_ENTRY_FULL) != RC_OK) return 0;
   BwdParams p;
   const int64_t bh = int64_t(B) * H;
-  if (plan_bwd(L, bh, p) != RC_OK) return 0;
+  if (plan_bwd(L, bh, D, p) != RC_OK) return 0;
   return 2 * bwd_row_bytes(bh * count_rows(L, RowSet::All)) + bwd_partial_bytes(p, bh, D);
 }
 
@@ -1059,7 +1073,7 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   const int64_t n = count_rows(L, RowSet::All), rows = int64_t(B) * H * n;
   BwdParams p;
   memset(&p, 0, sizeof p);
-  RC_TRY(plan_bwd(L, int64_t(B) * H, p));
+  RC_TRY(plan_bwd(L, int64_t(B) * H, D, p));
   RC_TRY(check_threads(int64_t(B) * H * p.n_pieces, 256, "attention gradient"));
   RC_TRY(check_threads((rows * (D / 8) + 255) / 256, 256, "attention gradient"));
   const size_t need = 2 * bwd_row_bytes(rows) + bwd_partial_bytes(p, int64_t(B) * H, D);

@@ -11,13 +11,16 @@
 // through one fp32 partial of dQ per 256 keys (two 1024-pixel samples of 24
 // heads: 7 GB written and read, 3 ms).  Two kinds of work-groups in one launch
 // compute seven products instead and write every output once: those that hold
-// 256 keys stream the queries that see them (S, dP, dV, dK), those that hold 256
-// queries stream the keys they see (S, dP, dQ).
+// 256 (128) keys stream the queries that see them (S, dP, dV, dK), those that hold
+// 256 (128) queries stream the keys they see (S, dP, dQ).
 //
 // Layout of the work.  A wave holds 64 own rows as two blocks of 32 (operands in
 // registers, sums in accumulation registers), so that a fragment read from LDS
 // feeds two products (one block and eight waves: 817 us for the ragged D = 64
-// case against 644).  Four waves share a 3-stage ring of 64 streamed rows of two
+// case against 644).  Few rows or heads take one block per wave and own tiles of 128
+// rows, on twice the work-groups: a tile's time falls to two thirds where a
+// work-group's time is the launch's (343 rows, one head: 21.5 -> 15.8 us; 22 heads of
+// 1516 rows 95.5 -> 103.8, so the planner weighs both).  Four waves share a 3-stage ring of 64 streamed rows of two
 // tensors, loaded straight to LDS (4 to 6 stages measured the same).  One wave
 // per SIMD, so nothing but its own order hides latency: the loop is one stream of
 // slots, each a product followed by its share of the other work (a fragment read
@@ -140,8 +143,8 @@ __device__ __forceinline__ void store_block(uint16_t* out, const f32x16& acc, fl
 template <int D, bool KV, int NB, int NW, int ST>
 __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const BwdSeg seg, int bh, int t, int piece) {
   using T = Bwd<D, KV, NB, NW, ST>;
-  // fragments read ahead of their MFMAs (D = 128 has no registers for a third)
-  constexpr int PF = D == 64 ? 3 : 2;
+  // fragments read ahead of their MFMAs (two blocks at D = 128 have no registers for a third)
+  constexpr int PF = NB == 1 ? 4 : D == 64 ? 3 : 2;
   constexpr int GR = T::GR, DC = T::DC, DB = T::DB, kT = T::kT;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -332,17 +335,19 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   const auto am = [](bf16x8 a, bf16x8 b, f32x16& c) {
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   };
-  // Score e = 0 .. 31 of the lane: the accumulators' first halves of both
+  // Score e = 0 .. 16 NB - 1 of the lane: the accumulators' first halves of the
   // blocks, then the second ones.  The argument of a score is computed kAhead
   // scores before its exponential.  (An empty statement that pins a value to
   // its place counts as its producer: the compiler puts a wait state between it
   // and a use right behind it.)
-  constexpr int kAhead = D == 64 ? 2 : 1;
+  constexpr int kAhead = D == 64 || NB == 1 ? 2 : 1;
   float arg[kAhead];
+  constexpr int NU = 16 * NB;
   const auto make_arg = [&](int e) {
-    const float x = s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)];
+    const int nb = (e >> 3) % NB;
+    const float x = s[nb][8 * (e / (8 * NB)) + (e & 7)];
     float& a = arg[e % kAhead];
-    a = KV ? x * p.scale_log2 : __builtin_fmaf(x, p.scale_log2, cs[(e >> 3) & 1]);
+    a = KV ? x * p.scale_log2 : __builtin_fmaf(x, p.scale_log2, cs[nb]);
     asm volatile("" : "+v"(a));
   };
   const auto first_args = [&] {
@@ -351,13 +356,13 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   };
   const auto unit = [&](int e) {
     float t = __builtin_amdgcn_exp2f(arg[e % kAhead]);
-    if (e + kAhead < 32) make_arg(e + kAhead);
+    if (e + kAhead < NU) make_arg(e + kAhead);
     asm volatile("" : "+v"(t));  // stays in its slot
-    s[(e >> 3) & 1][8 * (e >> 4) + (e & 7)] = t;
+    s[(e >> 3) % NB][8 * (e / (8 * NB)) + (e & 7)] = t;
   };
   const auto units = [&](int from, int to, int slot, int slots) {
 #pragma unroll
-    for (int e = 0; e < 32; ++e)
+    for (int e = 0; e < NU; ++e)
       if (e >= from && e < to && (e - from) * slots / (to - from) == slot) unit(e);
   };
   // dQ: scores of keys past the range are -inf (p = 0).  dK, dV need no mask:
@@ -373,7 +378,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
   };
   // Exponentials of a sub-block: kE1 beside dK (dQ) of the one before, up to
   // kE2 beside its dP, the rest beside the first half of its dV.
-  constexpr int kE1 = KV ? 11 : 16, kE2 = KV ? 24 : 32;
+  constexpr int kE1 = NU * (KV ? 11 : 16) / 32, kE2 = NU * (KV ? 24 : 32) / 32;
   constexpr int R = PF + 1;
   bf16x8 fr[R];
   uint32_t cur = 0, nxt = T::kStage, fill = (ST - 1) * T::kStage;
@@ -427,7 +432,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
       // is not computed in an earlier slot and other instructions lie in between.
       float dx[kAhead][2];
       const auto pin_pair = [&](int e) {
-        const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
+        const int ks = e / (4 * NB), nb = (e >> 2) % NB, r = 2 * (e & 3);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           dx[e % kAhead][i] = dp[nb][8 * ks + r + i];
@@ -440,16 +445,16 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
       };
       const auto ds = [&](int from, int to, int slot, int slots) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+        for (int e = 0; e < NU / 2; ++e)
           if (e >= from && e < to && (e - from) * slots / (to - from) == slot) {
-            const int ks = e >> 3, nb = (e >> 2) & 1, r = 2 * (e & 3);
+            const int ks = e / (4 * NB), nb = (e >> 2) % NB, r = 2 * (e & 3);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const float x = dx[e % kAhead][i];
               df[nb][ks][r + i] = (__bf16)(s[nb][8 * ks + r + i] * (kAdd ? x + cd[nb] : x));
             }
             asm volatile("" : "+v"(df[nb][ks]));
-            if (e + kAhead < 16) pin_pair(e + kAhead);
+            if (e + kAhead < NU / 2) pin_pair(e + kAhead);
           }
       };
       const auto next_tile = [&] {  // the next tile has landed everywhere, its stage's last readers are done
@@ -473,8 +478,8 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           fence();
           if (!KV && nb == 0 && g + PF == DC) next_tile();  // before the first read of S(i + 1)'s rows
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
-          units(kE1, kE2, 2 * c + nb, 2 * DC);
-          if (KV && 2 * c + nb >= 2 * DC - 4 && nb == 0) pack(0, c - (DC - 2));
+          units(kE1, kE2, NB * c + nb, NB * DC);
+          if (KV && nb == 0 && c >= DC - 2 && c - (DC - 2) < NB) pack(0, c - (DC - 2));
           fence();
         }
       }
@@ -489,10 +494,11 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
             am(fr[g % R], pf[nb][f / DB], acc2[nb][f % DB]);
             fence();
             if (nb == 0) fr[(g + PF) % R] = read(g + PF);
-            if (f < DB) units(kE2, 32, 2 * f + nb, 2 * DB);
-            else ds(0, 8, 2 * (f - DB) + nb, 2 * DB);
+            if (f < DB) units(kE2, NU, NB * f + nb, NB * DB);
+            else ds(0, NU / 4, NB * (f - DB) + nb, NB * DB);
             if (f == DB - 1) pack(1, nb);
-            if (f == DB - 1 && nb == 1) first_pairs();
+            if (f == DB - 1 && nb == NB - 1) first_pairs();
+            if (f == DB - 1 && NB == 1) asm volatile("s_nop 1");  // the next product reads what was just packed
             if (f == 2 * DB - 1 && nb == 0) nl = rows16(sn, sthere);
             fence();
           }
@@ -508,9 +514,9 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           s2[nb] = mm(fr[g % R], f1[nb][c], s2[nb]);
           fence();
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
-          if (KV) ds(8, 16, 2 * c + nb, DC);
-          else ds(0, 16, 2 * c + nb - 2, 2 * DC - 2);
-          if (!KV && c == 0 && nb == 1) first_pairs();
+          if (KV) ds(NU / 4, NU / 2, NB * c + nb, NB * DC / 2);
+          else ds(0, NU / 2, NB * c + nb - 2, NB * DC - 2);
+          if (!KV && c == 0 && nb == NB - 1) first_pairs();
           fence();
         }
       }
@@ -532,12 +538,12 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           fence();
           if (nb == 0) fr[(g + PF) % R] = read(g + PF);
           if (KV && f == 2 * DB - 2 && nb == 0) nd = rows16(sn, sthere + 256);
-          if (f == 0 && nb == 1) first_args();
-          units(0, kE1, 2 * f + nb - 2, 4 * DB - 2);
+          if (NB * f + nb == 1) first_args();
+          units(0, kE1, NB * f + nb - 2, 2 * NB * DB - 2);
           if (j == 1)
 #pragma unroll
             for (int l = 0; l < kLoads; ++l)
-              if (l * (4 * DB) / kLoads == 2 * f + nb) issue1(fill, l);
+              if (l * (2 * NB * DB) / kLoads == NB * f + nb) issue1(fill, l);
           fence();
         }
       }
@@ -569,10 +575,10 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
 
   const int lane_ = int(fresh_lane());
   if (seg.splits > 1) {  // a partial: 1 KB runs, in accumulator order
-    const int own_tiles = (seg.len + kBwdOwn - 1) / kBwdOwn;
+    const int own_tiles = (seg.len + T::kOwn - 1) / T::kOwn;
     const int64_t slot = int64_t(p.B) * p.H * seg.slot0 +
                          ((int64_t(bh) * own_tiles + t) * seg.splits + piece) * (KV ? 2 : 1);
-    f32x4* out = reinterpret_cast<f32x4*>(p.partial + slot * kBwdOwn * D) + lane_;
+    f32x4* out = reinterpret_cast<f32x4*>(p.partial + slot * T::kOwn * D) + lane_;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -584,7 +590,7 @@ __device__ __forceinline__ void bwd_tile(const BwdParams& p, char* ring, const B
           out[at] = f32x4{a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3]};
           if constexpr (KV) {
             const f32x16& c = acc2[nb][d];
-            out[at + kBwdOwn * D / 4] = f32x4{c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]};
+            out[at + T::kOwn * D / 4] = f32x4{c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]};
           }
         }
     return;
@@ -616,7 +622,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
   int si = 0;
   while (si + 1 < p.n_seg && p.seg[si + 1].piece0 * hx <= w) ++si;
   const BwdSeg seg = p.seg[si];
-  const int in_seg = w - seg.piece0 * hx, pieces = (seg.len + kBwdOwn - 1) / kBwdOwn * seg.splits;
+  constexpr int kOwn = Bwd<D, true, NB, NW, ST>::kOwn;
+  const int in_seg = w - seg.piece0 * hx, pieces = (seg.len + kOwn - 1) / kOwn * seg.splits;
   // (quotients come from vector instructions; as scalars they take no registers across the loops)
   const int head = __builtin_amdgcn_readfirstlane(in_seg / pieces), in_head = in_seg - head * pieces;
   const int t = __builtin_amdgcn_readfirstlane(in_head / seg.splits), piece = in_head - t * seg.splits;
@@ -629,9 +636,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void attn_bwd_kernel(const BwdPara
 // With few heads the split pays for it: five references, one head 897 us unsplit,
 // 335 split; a 512-pixel edit, three heads 142 and 64.  A wave takes one 32 x 32 block; its
 // partials' loads are in flight together, four pieces at a time.
-template <int D>
+template <int D, int kOwn>
 __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) {
-  constexpr int DB = D / 32, kBlocks = kBwdOwn / 32 * DB;  // blocks of one output of a tile
+  constexpr int DB = D / 32, kBlocks = kOwn / 32 * DB;  // blocks of one output of a tile
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   int64_t w = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t bhs = int64_t(p.B) * p.H;
@@ -639,7 +646,7 @@ __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) 
   int64_t own = 0;
   for (; si < p.n_seg; ++si) {
     if (p.seg[si].splits <= 1) continue;
-    own = (p.seg[si].len + kBwdOwn - 1) / kBwdOwn;
+    own = (p.seg[si].len + kOwn - 1) / kOwn;
     const int64_t n = bhs * own * (1 + p.seg[si].keys) * kBlocks;
     if (w < n) break;
     w -= n;
@@ -649,7 +656,7 @@ __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) 
   const int outs = 1 + seg.keys;
   const int block = int(w % kBlocks), out = int(w / kBlocks % outs);
   const int64_t tile = w / kBlocks / outs;  // (batch, head), own tile
-  const f32x4* src = reinterpret_cast<const f32x4*>(p.partial + (bhs * seg.slot0 + tile * seg.splits * outs + out) * kBwdOwn * D) +
+  const f32x4* src = reinterpret_cast<const f32x4*>(p.partial + (bhs * seg.slot0 + tile * seg.splits * outs + out) * kOwn * D) +
                      block * 256 + lane;
   f32x16 acc;
 #pragma unroll
@@ -660,14 +667,14 @@ __global__ __launch_bounds__(256) void attn_bwd_merge_kernel(const BwdParams p) 
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        v[j][i] = s0 + j < seg.splits ? src[int64_t(s0 + j) * outs * kBwdOwn * D / 4 + i * 64] : f32x4{};
+        v[j][i] = s0 + j < seg.splits ? src[int64_t(s0 + j) * outs * kOwn * D / 4 + i * 64] : f32x4{};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[r] += v[j][r / 4][r % 4];
   }
   const int64_t bh = tile / own;
-  const int r = int(tile % own) * kBwdOwn + block / DB * 32 + (lane & 31);
+  const int r = int(tile % own) * kOwn + block / DB * 32 + (lane & 31);
   uint16_t* dst = seg.keys ? (out ? p.dv : p.dk) : p.dq;
   dst += ((bh / p.H) * p.n_rows + seg.row0 + r) * p.g_st + (bh % p.H) * D + block % DB * 32 + 8 * hh;
   store_block(dst, acc, seg.keys && out ? 1.f : p.scale, r < seg.len);
@@ -698,27 +705,26 @@ __global__ __launch_bounds__(256) void attn_bwd_rows_kernel(const BwdParams p) {
   p.ndelta[at] = none ? 0.f : (p.dlse ? p.dlse[at] : 0.f) - s;
 }
 
-template <int D>
+template <int D, int NB>
 void launch(const BwdParams& p, hipStream_t s) {
+  constexpr int NW = 4, ST = 3, kOwn = 32 * NB * NW;
   const int64_t rows = int64_t(p.B) * p.n_rows * p.H;
   hipLaunchKernelGGL(attn_bwd_rows_kernel<D>, dim3((rows * (D / 8) + 255) / 256), dim3(256), 0, s, p);
   const int64_t bh = int64_t(p.B) * p.H;
-  constexpr int NB = 2, NW = kBwdOwn / 32 / NB, ST = 3;
-  hipLaunchKernelGGL((attn_bwd_kernel<D, NB, NW, ST>), dim3(bh * p.n_pieces),
-                     dim3(64 * NW), 0, s, p);
+  hipLaunchKernelGGL((attn_bwd_kernel<D, NB, NW, ST>), dim3(bh * p.n_pieces), dim3(64 * NW), 0, s, p);
   int64_t tiles = 0;
   for (int i = 0; i < p.n_seg; ++i)
-    if (p.seg[i].splits > 1) tiles += (p.seg[i].len + kBwdOwn - 1) / kBwdOwn * (1 + p.seg[i].keys);
+    if (p.seg[i].splits > 1) tiles += (p.seg[i].len + kOwn - 1) / kOwn * (1 + p.seg[i].keys);
   if (tiles > 0)  // four blocks of 32 x 32 per work-group
-    hipLaunchKernelGGL(attn_bwd_merge_kernel<D>, dim3(bh * tiles * (kBwdOwn * D / 4096)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((attn_bwd_merge_kernel<D, kOwn>), dim3(bh * tiles * (kOwn * D / 4096)), dim3(256), 0, s, p);
 }
 
 }  // namespace
 
 int launch_attention_bwd(const BwdParams& p, int D, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (D == 64) launch<64>(p, s);
-  else launch<128>(p, s);
+  if (p.own == 128) D == 64 ? launch<64, 1>(p, s) : launch<128, 1>(p, s);
+  else D == 64 ? launch<64, 2>(p, s) : launch<128, 2>(p, s);
   return int(hipGetLastError());
 }
 

@@ -22,12 +22,11 @@ struct BwdSeg {
   int32_t r0, nr;     // streamed ranges
   int32_t keys;       // own rows are keys
   int32_t splits;     // pieces of a tile's streamed rows; > 1: fp32 partials, merged by a second launch
-  int32_t slot0;      // first partial, per (batch, head), in units of one output's 256 x D
+  int32_t slot0;      // first partial, per (batch, head), in units of one output's own x D
 };
 struct BwdRange {
   int32_t start, len;
 };
-constexpr int kBwdOwn = 256;  // own rows of a tile
 
 struct BwdParams {
   const uint16_t* q;
@@ -45,7 +44,8 @@ struct BwdParams {
   int64_t st, g_st;    // token strides (elements) of Q/K/V and of the gradients; batch stride N times that
   int32_t B, H, n_rows;
   float scale, scale_log2;
-  float* partial;      // [slots B H, 256, D] in accumulator order
+  float* partial;      // [slots B H, own, D] in accumulator order
+  int32_t own;         // own rows of a tile: 256, or 128
   int32_t n_seg, n_pieces, n_slots;
   BwdSeg seg[2 * RC_MAX_SEGMENTS];
   BwdRange range[2 * kMaxRanges];

@@ -9,7 +9,7 @@
 
 namespace {
 
-long g_pieces = 0, g_slots = 0, g_chunks = 0, g_launches = 0;
+long g_pieces = 0, g_slots = 0, g_own = 0, g_chunks = 0, g_launches = 0;
 long g_pairs[2] = {0, 0};
 
 [[noreturn]] void fail(const char* what, long a, long b) {
@@ -28,6 +28,7 @@ namespace rc {
 
 int launch_attention_bwd(const BwdParams& p, int D, void*) {
   REQUIRE(D == 64 || D == 128, D, 0);
+  REQUIRE(p.own == 128 || p.own == 256, p.own, 0);
   REQUIRE(p.n_seg >= 1 && p.n_seg <= 2 * RC_MAX_SEGMENTS, p.n_seg, 0);
   REQUIRE(p.q && p.k && p.v && p.o && p.d_o && p.lse && p.dq && p.dk && p.dv && p.nlse && p.ndelta && p.partial, 0, 0);
   REQUIRE(isfinite(p.scale) && p.scale > 0 && fabsf(p.scale_log2 - p.scale * 1.44269504f) <= 1e-6f * p.scale_log2, 0, 0);
@@ -44,7 +45,7 @@ int launch_attention_bwd(const BwdParams& p, int D, void*) {
     REQUIRE(s.splits >= 1, i, s.splits);
     REQUIRE(s.piece0 == pieces && s.slot0 == slots, s.piece0, s.slot0);
     REQUIRE(s.nr >= 0 && s.r0 >= s.keys * kMaxRanges && s.r0 + s.nr <= (s.keys + 1) * kMaxRanges, s.r0, s.nr);
-    const int own = (s.len + kBwdOwn - 1) / kBwdOwn;
+    const int own = (s.len + p.own - 1) / p.own;
     long tiles = 0, end = 0;
     for (int r = 0; r < s.nr; ++r) {
       const BwdRange& g = p.range[s.r0 + r];
@@ -70,6 +71,7 @@ int launch_attention_bwd(const BwdParams& p, int D, void*) {
   REQUIRE(g_pairs[0] == g_pairs[1], g_pairs[0], g_pairs[1]);
   g_pieces = pieces;
   g_slots = slots;
+  g_own = p.own;
   ++g_launches;
   return 0;
 }
@@ -127,6 +129,7 @@ extern "C" {
 long rc_stub_layer_launches() { return g_launches; }
 long rc_stub_layer_pieces() { return g_pieces; }
 long rc_stub_layer_slots() { return g_slots; }
+long rc_stub_layer_own() { return g_own; }
 long rc_stub_layer_pairs(int keys) { return g_pairs[keys]; }
 long rc_stub_layer_chunks() { return g_chunks; }
 }
