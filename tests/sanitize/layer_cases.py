@@ -41,6 +41,17 @@ def test_random_layouts(preset):
     assert split > 20, "few layouts of the draw are split or have small own tiles"
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_own_tiles(D):
+    """Large ones where heads fill the chip, small ones for few rows or heads (test_gpu_backward.py relies on both)."""
+    layouts = [([(2, n)], "dense") for n in (129, 160, 191, 193, 224, 255, 256, 257, 320, 513)]
+    layouts += [([(0, 257), (1, 33), (2, 300), (3, 255), (3, 1)], p) for p in ("perref", "paper", "isolated", "dense")]
+    for segs, preset in layouts:
+        L = rc.Layout(segs, preset)
+        assert bwd(L, B=2, H=128, D=D, wsb=1 << 40) == rc.RC_OK and stub("own") == 256, (segs, preset)
+        assert bwd(L, B=1, H=2, D=D, wsb=1 << 40) == rc.RC_OK and stub("own") == 128, (segs, preset)
+
+
 def test_largest_table():
     L = rc.Layout([(2, 300)] * 32, "dense")
     assert bwd(L, wsb=1 << 40) == rc.RC_OK

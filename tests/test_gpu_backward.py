@@ -180,6 +180,27 @@ def test_many_work_groups(preset, D):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("segs,preset", [([(2, n)], "dense") for n in (129, 160, 191, 193, 224, 255, 256, 257, 320, 513)] +
+                         [([(0, 257), (1, 33), (2, 300), (3, 255), (3, 1)], p) for p in PRESETS],
+                         ids=lambda x: x if isinstance(x, str) else "-".join(str(n) for _, n in x))
+def test_many_heads_take_large_own_tiles(segs, preset, D):
+    """Enough heads that own tiles of 256 rows are chosen (as the planner's host test asserts): some of the
+    heads against the formula, all of them the same bits again and in strided outputs."""
+    L, B, H = rc.Layout(segs, preset), 2, 128
+    q, k, v, o, lse, do, dl = _inputs(L, B, H, D, seed=41, dlse=True)
+    got = rc.full_attention_backward(L, q, k, v, o, lse, do, dlse=dl)
+    pick = [0, 51, 127]
+    ref, tol = _reference(L, *(t[:, :, pick] for t in (q, k, v, o)), lse[:, pick], do[:, :, pick], dl[:, pick], D ** -0.5)
+    for name, g, r, t in zip(("dq", "dk", "dv"), got, ref, tol):
+        assert torch.isfinite(g).all(), name
+        over = ((g[:, :, pick].double() - r).abs() / t).max().item()
+        assert over <= 1.0, (name, over)
+    buf = torch.full((B, q.shape[1], 3, H, D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    for a, b in zip(rc.full_attention_backward(L, q, k, v, o, lse, do, *buf.unbind(2), dlse=dl), got):
+        assert torch.equal(a, b)
+
+
 def test_finite_differences():
     """sum(w O) + sum(u lse) along random directions, in 64 bits, against the kernel's gradient of them."""
     L = rc.Layout([(0, 5), (1, 40), (2, 70), (3, 33)], "paper")
