@@ -17,17 +17,17 @@
 // Layout of the work.  A wave holds 64 own rows as two blocks of 32 (operands in
 // registers, sums in accumulation registers), so that a fragment read from LDS
 // feeds two products (one block and eight waves: 817 us for the ragged D = 64
-// case against 644).  Few rows or heads take one block per wave and own tiles of 128
-// rows, on twice the work-groups: a tile's time falls to two thirds where a
-// work-group's time is the launch's (343 rows, one head: 21.5 -> 15.8 us; 22 heads of
-// 1516 rows 95.5 -> 103.8, so the planner weighs both).  Four waves share a 3-stage ring of 64 streamed rows of two
-// tensors, loaded straight to LDS (4 to 6 stages measured the same).  One wave
-// per SIMD, so nothing but its own order hides latency: the loop is one stream of
-// slots, each a product followed by its share of the other work (a fragment read
-// PF products ahead, one or two exponentials, a pair of ds, a load of the next
-// stage), and fences keep the compiler from moving work between slots.  The
-// scores of the next 32 rows are computed before dK (dQ) of the present ones, so
-// that their exponentials have products to hide behind.
+// case against 644).  Few rows or heads take one block per wave and own tiles of
+// 128 rows on twice the work-groups, each tile in two thirds of the time (343 rows,
+// one head: 21.5 -> 15.8 us; but 22 heads of 1516 rows: 95.5 -> 103.8, so the planner
+// weighs both).  Four waves share a 3-stage ring of 64 streamed rows of two tensors,
+// loaded straight to LDS (4 to 6 stages measured the same).  One wave per SIMD, so
+// nothing but its own order hides latency: the loop is one stream of slots, each a
+// product followed by its share of the other work (a fragment read PF products
+// ahead, one or two exponentials, a pair of ds, a load of the next stage), and
+// fences keep the compiler from moving work between slots.  The scores of the next
+// 32 rows are computed before dK (dQ) of the present ones, so that their
+// exponentials have products to hide behind.
 //
 // Rounding: P and ds are rounded to bf16 (off by at most 2^-8 of each) as operands
 // of the products dV, dK and dQ; scores, exponentials, dP and all sums stay fp32.
