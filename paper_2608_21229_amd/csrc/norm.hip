@@ -26,11 +26,19 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ bf16x8 load8(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
+// Rows pass through once: the forward's stores and the gradient's loads do not
+// stay in the L2 (a step's norm 18.0 -> 16.4 us, the gradient of 1024-pixel rows 73.6 ->
+// 68.3; loads forward and stores backward gained nothing or lost).
+__device__ __forceinline__ bf16x8 load8_once(const uint16_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p));
+}
+template <bool ONCE>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   bf16x8 o;
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = (__bf16)v[e];
-  *reinterpret_cast<bf16x8*>(p) = o;
+  if constexpr (ONCE) __builtin_nontemporal_store(o, reinterpret_cast<bf16x8*>(p));
+  else *reinterpret_cast<bf16x8*>(p) = o;
 }
 
 // Sums over the T threads of a row.  Each array has two halves that take turns,
@@ -125,7 +133,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[i][e] += f * x[i][e];
-      if (in) store8(p.h_out.p + r * p.h_out.ld + g * 8, h[i]);
+      if (in) store8<true>(p.h_out.p + r * p.h_out.ld + g * 8, h[i]);
     }
   }
   if (!p.y.p) return;
@@ -172,7 +180,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[i][e] += float(w[e]);
     }
-    if (in) store8(p.y.p + r * p.y.ld + g * 8, h[i]);
+    if (in) store8<true>(p.y.p + r * p.y.ld + g * 8, h[i]);
   }
 }
 
@@ -220,11 +228,11 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
       ry[i] = rn[i] = rh[i] = rx[i] = bf16x8{};
       if (!has[i] || i0 + rb >= count) continue;  // rows past the chunk are zeros and add nothing
       if (dy_) {
-        rn[i] = load8(p.h.p + r * p.h.ld + c);
-        ry[i] = load8(p.dy.p + r * p.dy.ld + c);
+        rn[i] = load8_once(p.h.p + r * p.h.ld + c);
+        ry[i] = load8_once(p.dy.p + r * p.dy.ld + c);
       }
-      if (dh_) rh[i] = load8(p.dh.p + r * p.dh.ld + c);
-      if (x_) rx[i] = load8(p.x.p + r * p.x.ld + c);
+      if (dh_) rh[i] = load8_once(p.dh.p + r * p.dh.ld + c);
+      if (x_) rx[i] = load8_once(p.x.p + r * p.x.ld + c);
     }
   };
   if constexpr (kAhead) load_rows(0);
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     if (in) {
 #pragma unroll
       for (int i = 0; i < GP; ++i)
-        if (has[i]) store8(p.dh_in.p + r * p.dh_in.ld + (t + i * T) * 8, dh[i]);
+        if (has[i]) store8<false>(p.dh_in.p + r * p.dh_in.ld + (t + i * T) * 8, dh[i]);
     }
     if (!x_) continue;
     float k[3] = {0.f, 0.f, 0.f}, rq = 1.f, dot = 0.f;
@@ -341,7 +349,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
         a_gate[i][e] += dh[i][e] * (x * gq);
         o[e] = rq * (dh[i][e] * w[at_vec(0, e)] - x * dot);
       }
-      if (in && has[i]) store8(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
+      if (in && has[i]) store8<false>(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
     }
   }
   // the row groups' sums, in order, through LDS
