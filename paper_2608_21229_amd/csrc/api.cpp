@@ -644,7 +644,7 @@ rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, con
 
 // Row groups per wave: whole tokens (their sines are computed once) as long as
 // that leaves 16 waves per CU, fewer for few tokens.  4608 tokens of 24 heads take
-// 20.8 us with 16 or 4 waves, 26.4 with 64; 512 tokens 11.8 with either.
+// 20.6 us with 16 waves, 24.7 with 64; 512 tokens 11.4 with either.
 int32_t rotary_groups(const RotaryParams& p, int32_t D) {
   const int rw = 512 / D;
   const int64_t all = int64_t(p.H + rw - 1) / rw * (p.x[0] && p.x[1] ? 2 : 1);

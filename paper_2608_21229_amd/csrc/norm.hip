@@ -12,7 +12,7 @@
 // pass over the registers (the row is in them); each output is rounded once.
 //
 // HBM-bound: every row is read once and written once.  4608 rows of 2560 channels
-// forward 17 us (94 MB, partly from cache); 8768 rows backward 59 us (269 MB, 4.6
+// forward 16 us (94 MB, partly from cache); 8768 rows backward 60 us (269 MB, 4.5
 // TB/s) and 6.5 us for the gradients shared by the rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -27,8 +27,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ bf16x8 load8(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
 // Rows pass through once: the forward's stores and the gradient's loads do not
-// stay in the L2 (a step's norm 18.0 -> 16.4 us, the gradient of 1024-pixel rows 73.6 ->
-// 68.3; loads forward and stores backward gained nothing or lost).
+// stay in the caches (new rows each call: a step's norm 18.0 -> 16.4 us, the gradient
+// of 1024-pixel rows 73.6 -> 68.3; loads forward and stores backward gained nothing or
+// lost.  A gradient called again on rows that the last-level cache would have kept
+// loses: 10877 rows of 1928 57 -> 65).
 __device__ __forceinline__ bf16x8 load8_once(const uint16_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p));
 }
@@ -466,14 +468,14 @@ void launch_bwd(const NormParams& p, hipStream_t s) {
 // Threads per row and granules per thread, by the row's granules.  A row inside
 // one wave needs no barrier; with more than two or three granules a thread the
 // registers leave too few waves and loads.  21 M values, us with 64, 128 and 256
-// threads a row:
+// threads a row (one set of rows again and again):
 //   C           512    1024    1928    2560    4096
-//   forward    28.8    27.4    29.1    28.6    36.1
-//              33.1    28.6    28.4    26.7    27.9
-//              45.5    32.3    28.4    27.8    27.4
-//   backward   53.9    54.9    59.0   128.1       -
-//              82.3    60.4    57.2    61.5    60.4
-//             141.2    88.5    58.5    66.8    55.2
+//   forward    28.6    26.9    30.4    26.8    33.3
+//              33.5    28.7    28.1    25.6    26.4
+//              46.1    32.7    29.7    26.1    26.5
+//   backward   56.4    57.4    64.4   125.6       -
+//              88.9    65.5    66.1    65.3    67.2
+//             156.2    91.1    71.0    68.5    64.4
 int launch_norm(const NormParams& p, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int ng = p.C / 8;

@@ -9,8 +9,8 @@
 // output is rounded once.
 //
 // HBM-bound: every row is read and written once: 4608 tokens of 24 heads, D = 128,
-// with the norm 21 us (113 MB); 2 x 7801 tokens of 12 heads backward 71 us (288 MB,
-// 4.1 TB/s) and 4 us for dw.  A head row is D / 8 lanes of 16
+// with the norm 20 us (113 MB); 2 x 7801 tokens of 12 heads backward 68 us (288 MB,
+// 4.2 TB/s) and 4 us for dw.  A head row is D / 8 lanes of 16
 // bytes, so a wave holds 512 / D head rows; it takes a token's rows of one
 // tensor after another, kAhead loads in flight, with the token's sines and
 // cosines (and the norm's weights) in registers.  out[e] = r (x[e] A[e] + x'[e] B[e])
@@ -32,8 +32,10 @@ constexpr int kAhead = 4;  // row groups loaded together
 
 __device__ __forceinline__ u32x4 load16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
 // Rows pass through once: the forward's stores and the gradient's loads do not
-// stay in the L2 (a step's rotation 23.1 -> 20.3 us, the video's gradient 81.9 -> 77.1;
-// loads forward and stores backward gained nothing or lost).
+// stay in the caches (new rows each call: a step's rotation 23.1 -> 20.3 us, the video's
+// gradient 81.9 -> 73.9; loads forward and stores backward gained nothing or lost.  A
+// gradient called again on rows that the last-level cache would have kept loses: 4608
+// tokens of 24 heads 36 -> 41).
 __device__ __forceinline__ u32x4 load16_once(const uint16_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
@@ -170,8 +172,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
 
 // Backward with a norm: a work-group takes a contiguous run of tokens, its
 // waves every fourth of them, and leaves its sums of dw.  Three work-groups per CU
-// (their registers' limit): 4608 x 24 and 15602 x 12 head rows take 36.4 and 58.4 us with
-// 768, 42.9 and 80.0 with 256, 47.8 and 69.6 with 1024, whose last 256 run alone.
+// (their registers' limit): 4608 x 24 and 15602 x 12 head rows take 41.4 and 61.5 us with
+// 768, 51.9 and 79.4 with 256, 55.2 and 72.7 with 1024, whose last 256 run alone.
 template <int D, bool HALVES>
 __global__ __launch_bounds__(256, 3) void rotary_norm_backward_kernel(const RotaryParams p) {
   constexpr int L = D / 8, RW = 64 / L;
