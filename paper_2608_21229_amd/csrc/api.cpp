@@ -629,6 +629,7 @@ rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, con
   p.H = H;
   p.axes = R->n_axes;
   p.eps = eps;
+  p.width = R->width;
   p.half = R->interleaved ? 0 : R->width / 2;
   for (int i = 0; i < R->head_dim / 2; ++i) {
     const bool in = 2 * i < R->width;

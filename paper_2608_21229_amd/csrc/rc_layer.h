@@ -67,6 +67,7 @@ struct RotaryParams {
   int32_t groups;         // row groups (64 lanes of 16 bytes each) per wave
   int32_t blocks;         // backward with a norm: work-groups of the first pass
   float eps, sign;        // sign: -1 turns back
+  int32_t width;          // rotated channels, the first ones of a head row
   int32_t half;           // > 0: channel p pairs with p + half; 0: 2p with 2p + 1
   uint8_t axis[64];
   double turns[64];       // per pair, revolutions per unit of position; 0 past the rotated width

@@ -59,16 +59,27 @@ __device__ __forceinline__ int partner(const RotaryParams& p, int lane, int g) {
   const int hg = p.half / 8;
   return 4 * (lane + (g < hg ? hg : g < 2 * hg ? -hg : 0));
 }
+// Whether the pair of a granule's channel e turns (with halves a granule turns
+// as a whole).  The channels past the rotated width stay what they are, whatever
+// else the row holds: a partner of zero, A = 1 and B = -0 for them.
 template <bool HALVES>
-__device__ __forceinline__ void partners(u32x4 raw, const float (&v)[8], int from, float (&o)[8]) {
+__device__ __forceinline__ bool turns(const RotaryParams& p, int g, int e) {
+  return g * 8 + (HALVES ? 0 : e & ~1) < p.width;
+}
+template <bool HALVES>
+__device__ __forceinline__ void partners(const RotaryParams& p, u32x4 raw, const float (&v)[8], int g, int from,
+                                         float (&o)[8]) {
   if constexpr (HALVES) {
     u32x4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ds_bpermute(from, int(raw[i]));
+    for (int i = 0; i < 4; ++i) {
+      r[i] = __builtin_amdgcn_ds_bpermute(from, int(raw[i]));
+      if (!turns<HALVES>(p, g, 0)) r[i] = 0;
+    }
     unpack(r, o);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = v[e ^ 1];
+    for (int e = 0; e < 8; ++e) o[e] = turns<HALVES>(p, g, e) ? v[e ^ 1] : 0.f;
   }
 }
 
@@ -97,16 +108,18 @@ __device__ __forceinline__ void angles(const RotaryParams& p, int64_t tok, int g
   for (int e = 0; e < 8; ++e) {
     A[e] = c[HALVES ? e : e / 2];
     B[e] = HALVES ? (g * 8 < p.half ? -s[HALVES ? e : 0] : s[HALVES ? e : 0]) : e & 1 ? s[e / 2] : -s[e / 2];
+    if (!turns<HALVES>(p, g, e)) A[e] = 1.f, B[e] = -0.f;
   }
 }
 
 // Weight of each channel into A, of its partner into B.
 template <bool HALVES>
-__device__ __forceinline__ void weigh(const uint16_t* w, int g, int from, float (&A)[8], float (&B)[8]) {
+__device__ __forceinline__ void weigh(const RotaryParams& p, const uint16_t* w, int g, int from, float (&A)[8],
+                                      float (&B)[8]) {
   const u32x4 raw = load16(w + g * 8);
   float v[8], o[8];
   unpack(raw, v);
-  partners<HALVES>(raw, v, from, o);
+  partners<HALVES>(p, raw, v, g, from, o);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     A[e] *= v[e];
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
       if (have != k) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) cA[e] = A[e], cB[e] = B[e];
-        if (w) weigh<HALVES>(w, g, from, cA, cB);
+        if (w) weigh<HALVES>(p, w, g, from, cA, cB);
         have = k;
       }
 #pragma unroll
@@ -153,7 +166,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
         if (j0 + j >= stop) continue;
         float v[8], o[8], r = 1.f;
         unpack(raw[j], v);
-        partners<HALVES>(raw[j], v, from, o);
+        partners<HALVES>(p, raw[j], v, g, from, o);
         if (w) {
           float ss = 0.f;
 #pragma unroll
@@ -218,7 +231,7 @@ __global__ __launch_bounds__(256, 3) void rotary_norm_backward_kernel(const Rota
           const int h = (j0 + j) * RW + sub;
           float u[8], o[8];
           unpack(rg[j], u);
-          partners<HALVES>(rg[j], u, from, o);
+          partners<HALVES>(p, rg[j], u, g, from, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e) o[e] = u[e] * A[e] + o[e] * B[e];
           if (w) {

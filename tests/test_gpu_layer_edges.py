@@ -1,0 +1,105 @@
+"""The rotation where values are not finite: what one channel or position holds
+reaches only the channels that the formula lets it reach.  Comparisons are of
+bits, or of which values are not finite; nothing here is rounded."""
+import pytest
+import torch
+
+import paper_2608_21229_amd as rc
+from synthgen import bf16_normal, derive_seed
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+INF, NAN = float("inf"), float("nan")
+
+
+def draw(shape, i, std=1.0):
+    return bf16_normal(tuple(shape), derive_seed(61, 0, 0, i), std).to(DEV)
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16)
+
+
+PARTIAL = [(64, (8, 20, 20)), (64, (4, 10, 8)), (128, (32, 48)), (128, (2, 0, 4)), (64, (0,))]
+
+
+def case(D, axes, interleaved, H=5):
+    if not interleaved:  # a rotated width that halves can have
+        axes = tuple(a // 16 * 16 for a in axes[:-1]) + (-(-axes[-1] // 16) * 16,)
+    R = rc.Rotary(D, axes, interleaved=interleaved)
+    pos = torch.arange(7 * len(axes), dtype=torch.int32, device=DEV).view(7, len(axes)) * 3 - 11
+    return R, sum(axes), draw((2, 7, H, D), 0), draw((2, 7, H, D), 1), pos
+
+
+def spoil(t, width):
+    """Values that are not finite, and a negative zero, in channels that do not turn."""
+    t = t.clone()
+    t[0, 1, 0, width + 1], t[0, 2, 4, width], t[1, 6, 3, -1], t[1, 0, 2, width + 2] = INF, NAN, -INF, -0.0
+    return t
+
+
+@pytest.mark.parametrize("D,axes", PARTIAL)
+@pytest.mark.parametrize("interleaved", [True, False], ids=["pairs", "halves"])
+@pytest.mark.parametrize("back", [False, True], ids=["forward", "gradient"])
+def test_channels_past_the_rotated_width_stay(D, axes, interleaved, back):
+    R, width, q, k, pos = case(D, axes, interleaved)
+    run = (lambda *a: rc.qk_rotary_backward(*a)[:2]) if back else rc.qk_rotary
+    clean = run(R, q, k, pos)
+    q2, k2 = spoil(q, width), spoil(k, width)
+    for x, y, before in zip((q2, k2), run(R, q2, k2, pos), clean):
+        assert torch.equal(bits(y[..., :width]), bits(before[..., :width]))
+        rest, want = y[..., width:], x[..., width:]
+        assert torch.equal(rest.isnan(), want.isnan())
+        assert torch.equal(bits(rest.masked_fill(rest.isnan(), 1)), bits(want.masked_fill(want.isnan(), 1)))
+
+
+@pytest.mark.parametrize("D,axes", PARTIAL)
+@pytest.mark.parametrize("interleaved", [True, False], ids=["pairs", "halves"])
+def test_positions_that_are_not_finite(D, axes, interleaved):
+    """They spoil their own axis's channels of their own tokens."""
+    R, width, q, k, pos = case(D, axes, interleaved)
+    pos = pos.float()
+    clean = rc.qk_rotary(R, q, k, pos)
+    axis = next((i for i, a in enumerate(R.axes) if a), 0)
+    pos[2, axis], pos[5, axis] = INF, NAN
+    own = [p for p in range(width // 2) if R.c.axis[p] == axis]
+    cols = [c for p in own for c in ((2 * p, 2 * p + 1) if interleaved else (p, p + width // 2))]
+    for y, before in zip(rc.qk_rotary(R, q, k, pos), clean):
+        bad = torch.zeros_like(y, dtype=torch.bool)
+        for n in (2, 5):
+            bad[:, n, :, cols] = True
+        assert torch.equal(y.isnan(), bad)
+        assert torch.equal(bits(y.masked_fill(bad, 0)), bits(before.masked_fill(bad, 0)))
+
+
+@pytest.mark.parametrize("D,axes", PARTIAL)
+@pytest.mark.parametrize("interleaved", [True, False], ids=["pairs", "halves"])
+def test_norm_of_rows_with_an_infinity_past_the_width(D, axes, interleaved):
+    """The row's norm is infinite: zeros, and NaN where infinity meets its zero."""
+    R, width, q, k, pos = case(D, axes, interleaved)
+    w = 1 + draw((D,), 2, 0.2)
+    clean = rc.qk_rotary(R, q, k, pos, q_norm=w, k_norm=w)
+    q[1, 3, 4, width + 1] = INF
+    got = rc.qk_rotary(R, q, k, pos, q_norm=w, k_norm=w)
+    row = got[0][1, 3, 4]
+    assert row[width + 1].isnan() and row.isnan().sum() == 1 and (row[~row.isnan()] == 0).all()
+    got[0][1, 3, 4] = clean[0][1, 3, 4]
+    assert torch.equal(bits(got[0]), bits(clean[0])) and torch.equal(bits(got[1]), bits(clean[1]))
+
+
+@pytest.mark.parametrize("D,axes", PARTIAL)
+@pytest.mark.parametrize("interleaved", [True, False], ids=["pairs", "halves"])
+def test_norm_gradient_with_an_infinity_past_the_width(D, axes, interleaved):
+    """It is lost for its own row and its own channel of the weight, nothing else."""
+    R, width, q, k, pos = case(D, axes, interleaved, H=8)
+    w = 1 + draw((D,), 2, 0.2)
+    dq, dk = draw(q.shape, 3), draw(k.shape, 4)
+    clean = rc.qk_rotary_backward(R, dq, dk, pos, q=q, k=k, q_norm=w, k_norm=w)
+    dq[1, 3, 4, width + 1] = INF
+    got = rc.qk_rotary_backward(R, dq, dk, pos, q=q, k=k, q_norm=w, k_norm=w)
+    assert got[2][width + 1].isinf() and (got[2][width + 1] > 0) == (q[1, 3, 4, width + 1] > 0)
+    got[2][width + 1] = clean[2][width + 1]
+    got[0][1, 3, 4] = clean[0][1, 3, 4]
+    for a, b in zip(got, clean):
+        assert torch.equal(a, b)
