@@ -245,12 +245,12 @@ __global__ __launch_bounds__(256, 3) void rotary_norm_backward_kernel(const Rota
             }
             const float r = rsqrtf(group_sum<L>(ss) * (1.f / D) + p.eps);
             const float m = group_sum<L>(dot) * (1.f / D) * r * r;
-            const float rin = h < p.H ? r : 0.f;
+            if (h < p.H) {  // the lanes past the last head hold its row once more
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              dw[k][e] += o[e] * (x[e] * rin);
-              o[e] = r * (u[e] - x[e] * m);
+              for (int e = 0; e < 8; ++e) dw[k][e] += o[e] * (x[e] * r);
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = r * (u[e] - x[e] * m);
           }
           if (h < p.H) store8<false>(y + int64_t(h) * D, o);
         }

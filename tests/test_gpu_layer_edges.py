@@ -103,3 +103,15 @@ def test_norm_gradient_with_an_infinity_past_the_width(D, axes, interleaved):
     got[0][1, 3, 4] = clean[0][1, 3, 4]
     for a, b in zip(got, clean):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D,H", [(128, 5), (128, 1), (64, 9), (64, 15)])
+def test_norm_gradient_with_an_infinity_in_the_last_head(D, H):
+    """The lanes behind a token's last head row hold a copy of it, which adds nothing to the weight's gradient."""
+    R = rc.Rotary(D, (16,))
+    q, dq = draw((1, 3, H, D), 5), draw((1, 3, H, D), 6)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV).view(3, 1)
+    w = 1 + draw((D,), 2, 0.2)
+    q[0, 1, H - 1, D - 1], dq[0, 1, H - 1, D - 1] = -2.0, INF
+    got = rc.qk_rotary_backward(R, dq, None, pos, q=q, q_norm=w)[2]
+    assert got[D - 1] == -INF and got[:D - 1].isfinite().all()
