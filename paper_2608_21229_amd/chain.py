@@ -48,7 +48,8 @@ class Chain:
     """A stack of synthetic layers with fixed weights and block mask.
 
     w_qkv[l]: [3 H D, H D] bf16, w_o[l]: [H D, H D] bf16, on one GPU.
-    rotary: a Rotary, with positions [N, axes] of all tokens in sequence order;
+    rotary: a Rotary, with positions [N, axes] of all tokens in sequence order,
+    copied here (later writes to the caller's tensor change nothing);
     q_norms, k_norms: a [D] weight per layer; modulated: every call takes
     ``modulation`` [B, groups, layers, 3, H D] (shift, scale, gate per layer):
     one group for prefill and step, two (live, static) for full."""
@@ -80,8 +81,11 @@ class Chain:
             raise ValueError(f"positions must be [{layout.rows(rcb.ROWS_ALL)}, axes], got {tuple(positions.shape)}")
         self.rotary, self.q_norms, self.k_norms = rotary, q_norms, k_norms
         self.modulated, self.norm, self.eps = modulated, norm, eps
-        self._positions = {rcb.ROWS_ALL: positions}
+        self._positions = {}
         if positions is not None:
+            # a copy, as the gathered rows below are: the cached path and the recompute stay of one mind
+            positions = positions.clone(memory_format=rcb._torch().contiguous_format)
+            self._positions[rcb.ROWS_ALL] = positions
             for which in (rcb.ROWS_STATIC, rcb.ROWS_LIVE):
                 self._positions[which] = self._rows_of(positions, which)
             # gathered on the stream that is current here, read on every call's
