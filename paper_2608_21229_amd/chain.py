@@ -134,6 +134,14 @@ class Chain:
         with rcb._on(stream, dev):
             yield lambda *ts: [t.record_stream(caller) for t in ts]
 
+    def _read_positions(self, rows_kind: int, dev):
+        """Marks a call's positions as read on the stream that is current (with
+        stream= the call's): they belong to the constructor's, nobody but the
+        chain holds them, and it may be dropped before they have been read."""
+        t = self._positions.get(rows_kind)
+        if t is not None and t.device == dev:  # elsewhere: the rotation refuses them
+            t.record_stream(rcb._torch().cuda.current_stream(dev))
+
     def _check_rows(self, h, rows_kind: int):
         if h.dim() != 3 or h.shape[2] != self.C:
             raise ValueError(f"hidden state must be [B, N, {self.C}], got {tuple(h.shape)}")
@@ -166,14 +174,12 @@ class Chain:
         if self.rotary is None:
             return q, k
         q_norm, k_norm = self._norms(l)
-        positions = self._positions[rows_kind]
-        if stream is not None:  # the chain may be dropped while the stream still reads them
-            positions.record_stream(rcb._torch().cuda.current_stream(q.device))
-        return rcb.qk_rotary(self.rotary, q, k, positions, q_norm=q_norm, k_norm=k_norm, eps=self.eps,
+        return rcb.qk_rotary(self.rotary, q, k, self._positions[rows_kind], q_norm=q_norm, k_norm=k_norm, eps=self.eps,
                              q_out=q if q_out is None else q_out, k_out=k if k_out is None else k_out, stream=stream)
 
     def _layers(self, h, rows_kind, attend, collect, last_out, stream, modulation):
         B, N, qkv, o, work = self._buffers(h, rows_kind)
+        self._read_positions(rows_kind, h.device)
         mod = self._mod(modulation, rows_kind, B)
         if mod is not None:
             return self._modulated_layers(h, rows_kind, attend, collect, last_out, stream, mod, B, N, qkv, o, work)
@@ -300,6 +306,7 @@ class Chain:
         if tuple(dh.shape) != tuple(h.shape):
             raise ValueError(f"dh must be {tuple(h.shape)}, got {tuple(dh.shape)}")
         mod = self._mod(modulation, rcb.ROWS_ALL, B)
+        self._read_positions(rcb.ROWS_ALL, h.device)
         spans = self._spans(rcb.ROWS_ALL)
         norm = dict(norm=self.norm, eps=self.eps, spans=spans, stream=stream)
         kept, h = [], h.contiguous()
