@@ -249,9 +249,10 @@ def _tok_stride(*ts) -> int:
     strides = set()
     for t in ts:
         B, N, H, D = t.shape
-        if t.stride(3) != 1 or t.stride(2) != D or (B > 1 and t.stride(0) != N * t.stride(1)):
+        if t.stride(3) != 1 or t.stride(2) != D or (B > 1 and N > 1 and t.stride(0) != N * t.stride(1)):
             raise ValueError("Q/K/V must be [B, N, H, D] with D contiguous, head stride D and batch stride N*tok_stride")
-        strides.add(t.stride(1))
+        # of one token the batch stride is the token stride; no token, or one of one entry, is at any stride
+        strides.add(t.stride(1) if N > 1 else t.stride(0) if N == 1 and B > 1 else H * D)
     if len(strides) != 1:
         raise ValueError("Q, K and V must share one token stride")
     return strides.pop()
