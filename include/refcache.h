@@ -414,7 +414,7 @@ rc_status rc_qk_rotary_backward(const rc_rotary* R, int32_t B, int64_t N, int32_
                                 const void* q, const void* k, int64_t tok_stride, const void* q_norm,
                                 const void* k_norm, float eps, void* dq_in, void* dk_in, int64_t out_stride,
                                 float* dq_norm, float* dk_norm, void* workspace, size_t ws_bytes, void* stream);
-size_t rc_rotary_backward_workspace_bytes(const rc_rotary* R, int32_t B, int64_t N);
+size_t rc_rotary_backward_workspace_bytes(const rc_rotary* R, int32_t B, int64_t N);  /* 0 on invalid input */
 
 #define RC_NORM_LAYER 0  /* mean removed, no affine */
 #define RC_NORM_RMS 1
@@ -465,7 +465,7 @@ rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy,
                                  int64_t lddhi, void* dx, int64_t lddx, float* dgate, float* dscale, float* dshift,
                                  float* dweight, float* dpost_weight, void* workspace, size_t ws_bytes,
                                  void* stream);
-size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);
+size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);  /* 0 on invalid input */
 
 /* Bytes of the static device array (per GPU) behind
  * rc_step_masked_attention_noalloc: 128 MiB, enough for the balanced schedule

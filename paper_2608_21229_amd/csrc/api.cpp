@@ -582,6 +582,8 @@ constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 rc_status check_float_ptr(const float* p, const char* name) { return check_lse(p, name); }
 
+bool rotary_size(int32_t B, int64_t N) { return B >= 1 && B <= 65535 && N >= 0 && N <= (int64_t(1) << 31) / B - 1; }
+
 // What both directions of the rotation check, and the parameters they share.
 rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, const void* a, const void* b,
                         const char* names, const void* positions, int32_t pos_float, int32_t pos_batch,
@@ -594,7 +596,7 @@ rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, con
     set_error("head_dim %d is not supported (64 or 128)", R->head_dim);
     return RC_ERR_UNSUPPORTED;
   }
-  if (B < 1 || H < 1 || B > 65535 || H > 65535 || N < 0 || N > (int64_t(1) << 31) / B - 1) {
+  if (!rotary_size(B, N) || H < 1 || H > 65535) {
     set_error("B = %d, H = %d: each must be in [1, 65535]; N = %lld: B * N below 2^31", B, H, (long long)N);
     return RC_ERR_ARG;
   }
@@ -1182,7 +1184,7 @@ rc_status rc_qk_rotary(const rc_rotary* R, int32_t B, int64_t N, int32_t H, cons
 }
 
 size_t rc_rotary_backward_workspace_bytes(const rc_rotary* R, int32_t B, int64_t N) {
-  if (!R || (R->head_dim != 64 && R->head_dim != 128) || B < 1 || N < 0) return 0;
+  if (!R || (R->head_dim != 64 && R->head_dim != 128) || !rotary_size(B, N)) return 0;
   return size_t(rotary_blocks(B, N)) * 2 * R->head_dim * sizeof(float);
 }
 

@@ -1,5 +1,8 @@
 """Batches of no or one token each, as slices of longer ones: the binding's
-strides for them, and the rotation over them."""
+strides for them, and the rotation over them.  Sizes out of range in the
+rotation's workspace query."""
+import ctypes
+
 import pytest
 import torch
 
@@ -21,6 +24,15 @@ def test_token_stride_of_no_and_one_token():
     for bad in ((q[:, :2],), (q[:, :1], k[:, :1].contiguous()), (q[..., ::2],), (q.transpose(2, 3),)):
         with pytest.raises(ValueError):
             rcb._tok_stride(*bad)
+
+
+@pytest.mark.parametrize("B,N", [(70_000, 5), (0, 5), (-1, 5), (2, -1), (2, 1 << 31), (65_535, 1 << 48), (65_535, (1 << 63) - 1),
+                                 (1, (1 << 63) - 1)])
+def test_rotation_workspace_of_sizes_out_of_range(B, N):
+    R = rc.Rotary(64, (16, 24, 24))
+    query = rc.lib().rc_rotary_backward_workspace_bytes
+    assert query(ctypes.byref(R.c), B, N) == 0
+    assert query(ctypes.byref(R.c), 65_535, 30_000) == 768 * 2 * 64 * 4
 
 
 @pytest.mark.gpu
