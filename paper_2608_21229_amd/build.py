@@ -14,6 +14,11 @@ import subprocess
 import sys
 import tempfile
 
+if __package__:
+    from . import wait_states
+else:  # run as a file
+    import wait_states
+
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
@@ -24,6 +29,9 @@ SOURCES = ["layout.cpp", "api.cpp", "attn_fwd.hip", "attn_bwd.hip", "linear.hip"
 # The attention gradient keeps its output accumulators in accumulation registers
 # by its own statements; every other matrix product of it stays in vector ones.
 SOURCE_FLAGS = {"attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# Those statements' wait states depend on what the compiler schedules around them, so
+# every build checks the listing of the object that it links.
+CHECKED = ["attn_bwd.hip"]
 ARCH = "gfx950"
 
 
@@ -54,12 +62,26 @@ def _finish(cmd, proc, verbose: bool):
     return f"hipcc failed ({proc.returncode}):\n{errs}" if proc.returncode != 0 else None
 
 
+def _hazards(source: str, objects: str):
+    """What is wrong with the listing that was kept beside a checked source's object, or None."""
+    name = f"{os.path.splitext(source)[0]}-hip-amdgcn-amd-amdhsa-{ARCH}.s"
+    with open(os.path.join(objects, name)) as f:
+        products, faults = wait_states.scan(f)
+    if faults or not products:
+        return (f"{source}: {len(faults)} of {products} accumulator products written as assembly lack wait states in this "
+                f"compiler's schedule: {faults[:3]}")
+    return None
+
+
 def build(verbose: bool = False) -> str:
     start = lambda cmd: subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)  # noqa: E731
     with tempfile.TemporaryDirectory() as tmp:
         objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
-        cmds = [compile_command(s, o, "-c") for s, o in zip(SOURCES, objs)]
+        cmds = [compile_command(s, o, "-c", *(["--save-temps=obj"] if s in CHECKED else []))
+                for s, o in zip(SOURCES, objs)]
         failed = [_finish(c, p, verbose) for c, p in [(c, start(c)) for c in cmds]]
+        if not any(failed):
+            failed = [_hazards(s, tmp) for s in CHECKED]
         if not any(failed):
             link = [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", *objs, "-o", LIB + ".tmp"]
             failed = [_finish(link, start(link), verbose)]
