@@ -26,11 +26,15 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ bf16x8 load8(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
-// Rows pass through once: the forward's stores and the gradient's loads do not
-// stay in the caches (new rows each call: a step's norm 18.0 -> 16.4 us, the gradient
-// of 1024-pixel rows 73.6 -> 68.3; loads forward and stores backward gained nothing or
-// lost.  A gradient called again on rows that the last-level cache would have kept
-// loses: 10877 rows of 1928 57 -> 65).
+// What is not read again soon does not stay in the caches: the forward's h', which the
+// next residual reads, and the gradient's loads, also behind the projection that wrote dy
+// and before the one that reads dx (8768 rows of 2560: 494 -> 487 us for the three; new
+// rows each call, alone: 73.6 -> 68.3).  y stays, since a projection reads it next: norm
+// and projection of 4608 rows of 2560 take 173 us, 186 with y past the caches, two layers'
+// recompute of 8768 rows 2139 and 2168, though the norm alone then takes 20.4, not 19.5.
+// The forward's loads and the gradient's stores gained nothing or lost.  A gradient
+// called again on rows that the last-level cache would have kept loses: 10877 rows of
+// 1928 57 -> 65.
 __device__ __forceinline__ bf16x8 load8_once(const uint16_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p));
 }
@@ -182,7 +186,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[i][e] += float(w[e]);
     }
-    if (in) store8<true>(p.y.p + r * p.y.ld + g * 8, h[i]);
+    if (in) store8<false>(p.y.p + r * p.y.ld + g * 8, h[i]);
   }
 }
 
