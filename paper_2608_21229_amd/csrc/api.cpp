@@ -647,7 +647,11 @@ rc_status rotary_params(const rc_rotary* R, int32_t B, int64_t N, int32_t H, con
 
 // Row groups per wave: whole tokens (their sines are computed once) as long as
 // that leaves 16 waves per CU, fewer for few tokens.  4608 tokens of 24 heads take
-// 20.6 us with 16 waves, 24.7 with 64; 512 tokens 11.4 with either.
+// 20.6 us with 16 waves, 24.7 with 64; 512 tokens 11.4 with either.  At most 12, as
+// measured where a token has more: 16384 tokens of 40 heads of 128, 20 groups a token, take
+// 124.6 us in waves of 12 and 8, 130.7 in one of 20, 129.3 in waves of 6; 64 heads of 64
+// 96.2, 98.7 and 101.6 (4608 tokens of 40 heads 40.8, 40.3 and 39.9); 24 heads of 128, 12
+// groups, 76.3 and, in waves of 6, 78.1.
 int32_t rotary_groups(const RotaryParams& p, int32_t D) {
   const int rw = 512 / D;
   const int64_t all = int64_t(p.H + rw - 1) / rw * (p.x[0] && p.x[1] ? 2 : 1);
@@ -729,7 +733,9 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   p.inv_c = 1.f / float(d->C);
   // The backward's chunks, one work-group each and one work-group per CU:
   // rows per chunk such that all of them fit one round (every span ends with a
-  // shorter one), a multiple of the four rows a work-group takes together.
+  // shorter one).  A multiple of four: a work-group takes four rows together from 1032
+  // to 3072 channels, eight below (the last step of a chunk may then be half empty), two
+  // or one above.
   const int64_t rows = d->N * d->B;
   // Where entries and spans alone are more, a span is one chunk.
   int64_t per = std::max<int64_t>(8, (rows + kCUs - 1) / kCUs + 3) / 4 * 4;

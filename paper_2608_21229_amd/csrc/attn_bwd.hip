@@ -34,7 +34,8 @@
 // The statistics enter in fp32: keys start S from -lse / scale and dP from -D (a
 // row's value is the accumulator's first addend), queries subtract them.
 //
-// What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.66 ms, 967 TFLOP/s
+// What bounds it (two 1024-pixel samples, 24 heads, D = 128): 3.66 ms (to 3.84 on other
+// machines; 4.0 in a process's first calls, whose clock is lower), 967 TFLOP/s
 // of five products, 1350 of the seven computed, which is what a large library
 // matrix product reaches here; the matrix pipes are busy 71% of the cycles and the
 // clock falls to 1.7 GHz.  With exponentials, ds, fragment reads and loads taken out

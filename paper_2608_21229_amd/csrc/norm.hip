@@ -12,8 +12,8 @@
 // pass over the registers (the row is in them); each output is rounded once.
 //
 // HBM-bound: every row is read once and written once.  4608 rows of 2560 channels
-// forward 16 us (94 MB, partly from cache); 8768 rows backward 60 us (269 MB, 4.5
-// TB/s) and 6.5 us for the gradients shared by the rows.
+// forward 17 us (94 MB, partly from cache; 20 with six sets of rows in turn); 8768 rows
+// backward 62 us (269 MB, 4.3 TB/s) and 6.5 us for the gradients shared by the rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -196,8 +196,9 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 // factors of the column).  The chunk's vectors (1 + scale) w and a gate w_p lie in
 // LDS; the next rows are loaded before the present ones are computed, except
 // with 4 granules a thread, whose registers that would overflow (1280 rows of 16384
-// channels: 144 us, 90 without).  The vectors' planes keep LDS reads free of bank
-// conflicts (two samples' 3936 rows of 1928 channels: 59.6 -> 52.9 us with the sums).
+// channels: 144 us, 90 without; with the present loads 84).  The vectors' planes leave
+// an eighth of the LDS bank conflicts (two samples' 3936 rows of 1928 channels: 7.7 M
+// -> 0.9 M cycles, 59.6 -> 52.9 us with the sums).
 template <int T, int GP>
 __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) {
   constexpr int NT = 512;
@@ -480,6 +481,10 @@ void launch_bwd(const NormParams& p, hipStream_t s) {
 //   backward   56.4    57.4    64.4   125.6       -
 //              88.9    65.5    66.1    65.3    67.2
 //             156.2    91.1    71.0    68.5    64.4
+// Backward, 1032 to 2048 channels: 64 threads, 128 here, are better for many rows and
+// worse for few (new rows each call: 10877 rows of 1928 63.9 with 64, 65.8 with 128, 10877
+// of 1160 46.0 and 52.2, two samples' 3936 of 1928 55.1 and 57.6; but 1417 rows of 2048
+// 27.1 and 23.7, 80 rows 21.5 and 17.9).  128 lose at most 14%, 64 up to 20%.
 int launch_norm(const NormParams& p, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int ng = p.C / 8;

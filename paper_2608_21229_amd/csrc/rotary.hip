@@ -9,8 +9,8 @@
 // output is rounded once.
 //
 // HBM-bound: every row is read and written once: 4608 tokens of 24 heads, D = 128,
-// with the norm 20 us (113 MB); 2 x 7801 tokens of 12 heads backward 68 us (288 MB,
-// 4.2 TB/s) and 4 us for dw.  A head row is D / 8 lanes of 16
+// with the norm 20 us (113 MB, partly from cache; 24 with six sets of rows in turn); 2 x
+// 7801 tokens of 12 heads backward 71 us (288 MB, 4.1 TB/s) and 5 us for dw.  A head row is D / 8 lanes of 16
 // bytes, so a wave holds 512 / D head rows; it takes a token's rows of one
 // tensor after another, kAhead loads in flight, with the token's sines and
 // cosines (and the norm's weights) in registers.  out[e] = r (x[e] A[e] + x'[e] B[e])
