@@ -218,6 +218,8 @@ class Layout:
     def modulation_spans(self, which: int = ROWS_ALL, live: int = 0, static: int = 1):
         """(rows, group) spans of a row class for gated_norm: live segments
         (text, target) take group `live`, static ones (anchors, references) `static`."""
+        if which not in (ROWS_STATIC, ROWS_LIVE, ROWS_ALL):
+            raise ValueError(f"modulation spans are those of ROWS_STATIC, ROWS_LIVE or ROWS_ALL, got {which!r}")
         spans = []
         for k, n in self.segments:
             is_live = k in (SEG_TEXT, SEG_TARGET)
