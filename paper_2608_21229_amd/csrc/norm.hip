@@ -233,7 +233,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     for (int i = 0; i < GP; ++i) {
       const int c = (t + i * T) * 8;
       ry[i] = rn[i] = rh[i] = rx[i] = bf16x8{};
-      if (!has[i] || i0 + rb >= count) continue;  // rows past the chunk are zeros and add nothing
+      if (!has[i] || i0 + rb >= count) continue;  // zeros past the row's end and the chunk's
       if (dy_) {
         rn[i] = load8_once(p.h.p + r * p.h.ld + c);
         ry[i] = load8_once(p.dy.p + r * p.dy.ld + c);
@@ -243,20 +243,22 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     }
   };
   if constexpr (kAhead) load_rows(0);
-  for (int g = threadIdx.x; g < ng; g += NT) {
-    float s[8], a[8];
-    const bf16x8 vs = p.scale ? load8(p.scale + mod + g * 8) : bf16x8{};
+  for (int g = threadIdx.x; g < T * GP; g += NT) {  // zeros past the row's end, where its values are zeros, too
+    float s[8] = {}, a[8] = {};
+    if (g < ng) {
+      const bf16x8 vs = p.scale ? load8(p.scale + mod + g * 8) : bf16x8{};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = 1.f + float(vs[e]), a[e] = p.rscale;
-    const auto times = [&](float (&v)[8], const uint16_t* w) {
-      if (!w) return;
-      const bf16x8 x = load8(w + g * 8);
+      for (int e = 0; e < 8; ++e) s[e] = 1.f + float(vs[e]), a[e] = p.rscale;
+      const auto times = [&](float (&v)[8], const uint16_t* w) {
+        if (!w) return;
+        const bf16x8 x = load8(w + g * 8);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= float(x[e]);
-    };
-    times(s, p.weight);
-    times(a, p.gate ? p.gate + mod : nullptr);
-    times(a, p.post_weight);
+        for (int e = 0; e < 8; ++e) v[e] *= float(x[e]);
+      };
+      times(s, p.weight);
+      times(a, p.gate ? p.gate + mod : nullptr);
+      times(a, p.post_weight);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) vec[at_vec(g, e)] = s[e], vec[2 * kPlane + at_vec(g, e)] = a[e];
   }
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
       float k[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const float* w = vec + (has[i] ? (t + i * T) * 4 : 0);
+        const float* w = vec + (t + i * T) * 4;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float dn = d[i][e] * w[at_vec(0, e)];
@@ -310,16 +312,18 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
-      const float rs = in ? rsqrtf(k[0] * p.inv_c + p.eps) : 0.f;
+      const float rs = rsqrtf(k[0] * p.inv_c + p.eps);
       const float mean = p.rms ? 0.f : k[1] * p.inv_c, dot = k[2] * p.inv_c * rs * rs;
+      if (in) {  // a whole wave; rows past the chunk add nothing, whatever the vectors hold
 #pragma unroll
-      for (int i = 0; i < GP; ++i) {
-        const float* w = vec + (has[i] ? (t + i * T) * 4 : 0);
+        for (int i = 0; i < GP; ++i) {
+          const float* w = vec + (t + i * T) * 4;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          a_shift[i][e] += d[i][e];
-          a_scale[i][e] += d[i][e] * (n[i][e] * rs);
-          dh[i][e] += rs * (d[i][e] * w[at_vec(0, e)] - mean - n[i][e] * dot);
+          for (int e = 0; e < 8; ++e) {
+            a_shift[i][e] += d[i][e];
+            a_scale[i][e] += d[i][e] * (n[i][e] * rs);
+            dh[i][e] += rs * (d[i][e] * w[at_vec(0, e)] - mean - n[i][e] * dot);
+          }
         }
       }
     }
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
     if (p.post) {
 #pragma unroll
       for (int i = 0; i < GP; ++i) {
-        const float* w = vec + 2 * kPlane + (has[i] ? (t + i * T) * 4 : 0);
+        const float* w = vec + 2 * kPlane + (t + i * T) * 4;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float x = float(cx[i][e]);
@@ -342,13 +346,14 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
         }
       }
       row_sums<T, 3>(k, lds3, rb, half3);
-      rq = in ? rsqrtf(k[0] * p.inv_c + p.eps) : 0.f;
+      rq = rsqrtf(k[0] * p.inv_c + p.eps);
       dot = k[1] * p.inv_c * rq * rq;
     }
+    if (!in) continue;
     const float gq = rq * p.rscale;
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
-      const float* w = vec + 2 * kPlane + (has[i] ? (t + i * T) * 4 : 0);
+      const float* w = vec + 2 * kPlane + (t + i * T) * 4;
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -356,7 +361,7 @@ __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) 
         a_gate[i][e] += dh[i][e] * (x * gq);
         o[e] = rq * (dh[i][e] * w[at_vec(0, e)] - x * dot);
       }
-      if (in && has[i]) store8<false>(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
+      if (has[i]) store8<false>(p.dx.p + r * p.dx.ld + (t + i * T) * 8, o);
     }
   }
   // the row groups' sums, in order, through LDS
