@@ -40,7 +40,7 @@ def test_an_infinite_scale_in_a_chunk_that_ends_early(C, post, N, first):
     dh = r * (dn - n * dot)
     xn = x.double() * torch.rsqrt(x.double().square().mean(-1, keepdim=True) + 1e-6) if post else x.double()
     want = (dh * xn).sum((0, 1))
-    assert want.isinf().any()
+    assert N > 1 or want.isinf().sum() >= C - 1  # several rows may disagree in every sign
     assert torch.equal(got.gate[0, 0].isnan(), want.isnan())
     assert torch.equal(got.gate[0, 0].isinf(), want.isinf()) and torch.equal(got.gate[0, 0] > 0, want > 0)
     assert torch.equal(got.shift, clean.shift) and torch.equal(got.scale, clean.scale)
