@@ -29,9 +29,10 @@ With ``cache="fp8"`` each layer's reference cache is stored as e4m3 codes
 with per-(batch, head) scales (``ref_kv_prefill_fp8`` /
 ``step_masked_attention_fp8``); the computation stays bf16.
 
-Marshalling only: every multiply-add runs in librefcache.  Work buffers come
-from torch's allocator; ``collect`` (a list) receives a copy of the hidden
-state after each layer.  With ``stream`` given, everything that a call
+Every multiply-add runs in librefcache.  Work buffers come from torch's
+allocator; ``collect`` (a list) receives a copy of the hidden state after each
+layer.  ``full_backward`` also copies with torch: the weights transposed, and for
+the weights' gradients both activations of a product transposed and padded.  With ``stream`` given, everything that a call
 allocates, copies and launches is that stream's.
 """
 from __future__ import annotations

@@ -13,7 +13,7 @@
 //
 // HBM-bound: every row is read once and written once.  4608 rows of 2560 channels
 // forward 17 us (94 MB, partly from cache; 20 with six sets of rows in turn); 8768 rows
-// backward 62 us (269 MB, 4.3 TB/s) and 6.5 us for the gradients shared by the rows.
+// backward 61 us (269 MB, 4.4 TB/s) and 6.5 us for the gradients shared by the rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -196,9 +196,10 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormParams p) {
 // factors of the column).  The chunk's vectors (1 + scale) w and a gate w_p lie in
 // LDS; the next rows are loaded before the present ones are computed, except
 // with 4 granules a thread, whose registers that would overflow (1280 rows of 16384
-// channels: 144 us, 90 without; with the present loads 84).  The vectors' planes leave
-// an eighth of the LDS bank conflicts (two samples' 3936 rows of 1928 channels: 7.7 M
-// -> 0.9 M cycles, 59.6 -> 52.9 us with the sums).
+// channels: 144 us, 90 without; with the present loads 84).  The vectors' planes, and
+// zeros of their own for lanes past a row's end, leave few LDS bank conflicts (two samples'
+// 3936 rows of 1928 channels: 7.7 M -> 0.9 M -> 0.05 M cycles; 59.6 -> 52.9 us with the
+// sums, then 57.7 -> 56.7 with new rows each call).
 template <int T, int GP>
 __global__ __launch_bounds__(512) void norm_backward_kernel(const NormParams p) {
   constexpr int NT = 512;
