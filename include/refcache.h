@@ -306,7 +306,7 @@ size_t rc_full_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t
  * their o, d_o and dlse hold; keys that nobody reads get dk = dv = 0.
  * Deterministic: the sums keep one order.  RC_ERR_WORKSPACE for a missing or small workspace;
  * RC_ERR_UNSUPPORTED where the mask needs too many merged ranges from either side, and for a
- * scale below 2^-96. */
+ * scale below 2^-96; RC_ERR_ARG for launches of 2^32 threads and more (B H N D / 8). */
 rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, int32_t D, float scale,
                                      const void* q, const void* k, const void* v, int64_t tok_stride,
                                      const void* o, const float* lse, const void* d_o, const float* dlse,
@@ -314,8 +314,8 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
                                      void* workspace, size_t ws_bytes, void* stream);
 
 /* Bytes of workspace rc_full_attention_backward needs: two floats per (batch,
- * head, row), and fp32 partials where few heads split their sums.  0 on
- * invalid input. */
+ * head, row), and fp32 partials where few heads split their sums.  0 for what
+ * the call refuses by its layout or sizes. */
 size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H, int32_t D);
 
 /* FP8 reference cache (the paper calls caching complementary to other

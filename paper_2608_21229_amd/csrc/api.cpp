@@ -571,8 +571,26 @@ rc_status plan_bwd(const rc_layout* L, int64_t bh, int32_t D, BwdParams& b) {
   return RC_OK;
 }
 
+// A launch's threads are counted in 32 bits.
+rc_status check_threads(int64_t blocks, int64_t threads, const char* what) {
+  if (blocks > ((int64_t(1) << 32) - 1) / threads) {
+    set_error("%s launch of %lld x %lld threads exceeds the grid limit", what, (long long)blocks, (long long)threads);
+    return RC_ERR_ARG;
+  }
+  return RC_OK;
+}
+
 // lse / scale is a first addend of the recomputed scores and has to stay finite.
 constexpr float kBwdMinScale = 0x1p-96f;
+
+// The schedule of a call whose launches stay in their limits.  Rows first: they
+// bound the planner's costs, which overflow 64 bits at sizes that B, H and N alone allow.
+rc_status plan_bwd_launches(const rc_layout* L, int32_t B, int32_t H, int32_t D, BwdParams& p) {
+  const int64_t bh = int64_t(B) * H, rows = bh * count_rows(L, RowSet::All);
+  RC_TRY(check_threads((rows * (D / 8) + 255) / 256, 256, "attention gradient"));
+  RC_TRY(plan_bwd(L, bh, D, p));
+  return check_threads(bh * p.n_pieces, 256, "attention gradient");
+}
 
 size_t bwd_partial_bytes(const BwdParams& p, int64_t bh, int32_t D) {
   return size_t(bh) * p.n_slots * p.own * D * sizeof(float);
@@ -751,15 +769,6 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   for (int s = 0; s < p.n_spans; ++s) {
     p.span_chunk0[s] = p.chunks;
     p.chunks += (p.span_rows[s] + p.chunk_rows - 1) / p.chunk_rows;
-  }
-  return RC_OK;
-}
-
-// A launch's threads are counted in 32 bits.
-rc_status check_threads(int64_t blocks, int64_t threads, const char* what) {
-  if (blocks > ((int64_t(1) << 32) - 1) / threads) {
-    set_error("%s launch of %lld x %lld threads exceeds the grid limit", what, (long long)blocks, (long long)threads);
-    return RC_ERR_ARG;
   }
   return RC_OK;
 }
@@ -1048,7 +1057,7 @@ size_t rc_full_backward_workspace_bytes(const rc_layout* L, int32_t B, int32_t H
   if (check_layout(L, RC_ENTRY_FULL) != RC_OK) return 0;
   BwdParams p;
   const int64_t bh = int64_t(B) * H;
-  if (plan_bwd(L, bh, D, p) != RC_OK) return 0;
+  if (plan_bwd_launches(L, B, H, D, p) != RC_OK) return 0;
   return 2 * bwd_row_bytes(bh * count_rows(L, RowSet::All)) + bwd_partial_bytes(p, bh, D);
 }
 
@@ -1082,9 +1091,7 @@ rc_status rc_full_attention_backward(const rc_layout* L, int32_t B, int32_t H, i
   const int64_t n = count_rows(L, RowSet::All), rows = int64_t(B) * H * n;
   BwdParams p;
   memset(&p, 0, sizeof p);
-  RC_TRY(plan_bwd(L, int64_t(B) * H, D, p));
-  RC_TRY(check_threads(int64_t(B) * H * p.n_pieces, 256, "attention gradient"));
-  RC_TRY(check_threads((rows * (D / 8) + 255) / 256, 256, "attention gradient"));
+  RC_TRY(plan_bwd_launches(L, B, H, D, p));
   const size_t need = 2 * bwd_row_bytes(rows) + bwd_partial_bytes(p, int64_t(B) * H, D);
   if (!workspace || !aligned16(workspace) || ws_bytes < need) {
     set_error("the attention gradient needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
