@@ -50,7 +50,8 @@ class Chain:
 
     w_qkv[l]: [3 H D, H D] bf16, w_o[l]: [H D, H D] bf16, on one GPU.
     rotary: a Rotary, with positions [N, axes] of all tokens in sequence order,
-    copied here (later writes to the caller's tensor change nothing);
+    copied here (later writes to the caller's tensor change nothing; keep the
+    chain as long as a graph that captured its calls is replayed);
     q_norms, k_norms: a [D] weight per layer; modulated: every call takes
     ``modulation`` [B, groups, layers, 3, H D] (shift, scale, gate per layer):
     one group for prefill and step, two (live, static) for full."""
