@@ -751,9 +751,9 @@ rc_status norm_params(const rc_norm* d, NormParams& p) {
   p.inv_c = 1.f / float(d->C);
   // The backward's chunks, one work-group each and one work-group per CU:
   // rows per chunk such that all of them fit one round (every span ends with a
-  // shorter one).  A multiple of four: a work-group takes four rows together from 1032
-  // to 3072 channels, eight below (the last step of a chunk may then be half empty), two
-  // or one above.
+  // shorter one).  A multiple of four: a work-group takes four rows together where a row
+  // has 129 to 384 granules of 8 channels, eight below (the last step of a chunk may then be
+  // half empty), two or one above.
   const int64_t rows = d->N * d->B;
   // Where entries and spans alone are more, a span is one chunk.
   int64_t per = std::max<int64_t>(8, (rows + kCUs - 1) / kCUs + 3) / 4 * 4;
