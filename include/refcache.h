@@ -30,6 +30,8 @@
  *   rc_qk_rotary                RMS norm and rotation of queries and keys by position,
  *   rc_gated_norm               residual with a gated block output, norm and modulation,
  *                               each with its gradient (*_backward).
+ *   rc_linear_fp8               the projection in 8 bits, with its gradient; rc_quantize_blocks and
+ *                               rc_dequantize_blocks make and expand its weights and checkpoints.
  *
  * Common conventions
  *   Element type   bf16 for Q, K, V, O and the cache (passed as raw bits;
@@ -466,6 +468,63 @@ rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy,
                                  float* dweight, float* dpost_weight, void* workspace, size_t ws_bytes,
                                  void* stream);
 size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);  /* 0 on invalid input */
+
+/* ------------------------------------------------------------------------
+ * Projections in 8 bits.  A matrix [rows, cols] is held as e4m3fn codes with one
+ * power-of-two scale per block, the block of (row, col) being 128 values of a
+ * row, or a square of 128 x 128 (weights), of which all 128 rows then hold the
+ * same scale:
+ *   value(row, col) = e4m3(codes[row * ld + col]) * 2^(exps[col / 128 * ld_exps + row] - 127)
+ *   ld       bytes, >= cols rounded up to 128, a multiple of 16, <= 2^22; columns past the last up to
+ *            that multiple of 128 exist and hold zeros
+ *   ld_exps  bytes, >= rows rounded up to 16, a multiple of 16; what it holds past the rows is unspecified
+ * Quantisation: e is the smallest integer >= -127 with (largest finite magnitude of the block) * 2^-e <=
+ * 448, 0 where that is 0; the code is the e4m3fn value nearest to x * 2^-e (ties to even; the product is
+ * exact); infinities and NaN become NaN.
+ * Sizes: 0 <= rows <= 2^28, columns multiples of 8 from 8 to 2^22.  Pointers 16-byte aligned; row strides of
+ * bf16 and fp32 matrices in elements, multiples of 8, <= 2^22.  Outputs overlap no input except as said.
+ * RC_ERR_UNSUPPORTED for columns off those multiples, RC_ERR_ARG otherwise.  rows = 0 is a no-op. */
+typedef struct {
+  void* codes;
+  int64_t ld;
+  void* exps;
+  int64_t ld_exps;
+} rc_blocks8;
+
+/* x [M, K] bf16 to blocks; square: of 128 x 128.  out_t (square only, nullable): the transposed matrix
+ * [K, M] as well, whose values are the same (M <= 2^22 then, a multiple of 8). */
+rc_status rc_quantize_blocks(int64_t M, int32_t K, const void* x, int64_t ldx, int32_t square,
+                             const rc_blocks8* out, const rc_blocks8* out_t, void* stream);
+
+/* The values in bf16 (exact from 2^-133 on). */
+rc_status rc_dequantize_blocks(int64_t M, int32_t K, const rc_blocks8* x, void* out, int64_t ldo, void* stream);
+
+/* out[m, n] = bf16( sum_k a[m, k] w[n, k] (+ r[m, n]) ) of the values of a [M, K] and w [N, K], fp32
+ * accumulation in a fixed order, one RNE rounding.  A row's result depends on its own values only and is
+ * the same for every M.  r nullable; out may be r (same stride). */
+rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8* a, const rc_blocks8* w,
+                               const void* r, int64_t ldr, void* out, int64_t ldo, void* stream);
+
+/* The same of the quantised rows of a [M, K] bf16 (blocks of a row), without handing them out.  The
+ * workspace (rc_linear_fp8_workspace_bytes, 16-byte aligned) holds them; up to 16 rows need none and are
+ * summed in another order than by rc_linear_fp8_blocks. */
+rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const rc_blocks8* w,
+                        const void* r, int64_t ldr, void* out, int64_t ldo, void* workspace, size_t ws_bytes,
+                        void* stream);
+size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K);  /* 0 on invalid input, too */
+
+/* The gradient of rc_linear_fp8_blocks for dy [M, N] bf16.
+ *   dx [M, K] bf16  = sum_n dy[m, n] w[n, k] (+ r[m, k]): rc_linear_fp8 of dy, quantised in blocks of a row,
+ *                     and w_t, the transposed weights [K, N]; NULL: not wanted, w_t and r are then NULL
+ *   dw [N, K] fp32  = sum_m dy[m, n] x[m, k], of dy as it is and of the values of x [M, K], the product's input,
+ *                     which is its own checkpoint; zeros for M = 0; NULL: not wanted, x is then NULL
+ * r may be dx (same stride).  Workspace: rc_linear_fp8_backward_workspace_bytes bytes for the same wishes, 16-byte
+ * aligned.  Deterministic: the sums over rows keep one order. */
+rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy, int64_t lddy,
+                                 const rc_blocks8* x, const rc_blocks8* w_t, const void* r, int64_t ldr, void* dx,
+                                 int64_t lddx, float* dw, int64_t lddw, void* workspace, size_t ws_bytes,
+                                 void* stream);
+size_t rc_linear_fp8_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t want_dx, int32_t want_dw);
 
 /* Bytes of the static device array (per GPU) behind
  * rc_step_masked_attention_noalloc: 128 MiB, enough for the balanced schedule

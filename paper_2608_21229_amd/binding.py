@@ -59,6 +59,11 @@ class rc_rotary(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64), ("turns", ctypes.c_double * 64)]
 
 
+class rc_blocks8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_int64), ("exps", ctypes.c_void_p),
+                ("ld_exps", ctypes.c_int64)]
+
+
 class rc_norm(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("C", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("norm", ctypes.c_int32),
                 ("post", ctypes.c_int32), ("N", ctypes.c_int64), ("eps", ctypes.c_float),
@@ -71,6 +76,7 @@ _LIB = None
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 _f64 = ctypes.c_double
 _PL, _PR, _PN = ctypes.POINTER(rc_layout), ctypes.POINTER(rc_rotary), ctypes.POINTER(rc_norm)
+_PB = ctypes.POINTER(rc_blocks8)
 SIGNATURES = {
     "rc_layout_preset": (_i32, [_PL, _i32]),
     "rc_layout_validate": (_i32, [_PL, _i32]),
@@ -109,6 +115,14 @@ SIGNATURES = {
     "rc_gated_norm_backward_workspace_bytes": (_sz, [_PN]),
     "rc_gated_norm_backward": (_i32, [_PN, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64,
                                       _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "rc_quantize_blocks": (_i32, [_i64, _i32, _vp, _i64, _i32, _PB, _PB, _vp]),
+    "rc_dequantize_blocks": (_i32, [_i64, _i32, _PB, _vp, _i64, _vp]),
+    "rc_linear_fp8_blocks": (_i32, [_i64, _i32, _i32, _PB, _PB, _vp, _i64, _vp, _i64, _vp]),
+    "rc_linear_fp8": (_i32, [_i64, _i32, _i32, _vp, _i64, _PB, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "rc_linear_fp8_workspace_bytes": (_sz, [_i64, _i32, _i32]),
+    "rc_linear_fp8_backward": (_i32, [_i64, _i32, _i32, _vp, _i64, _PB, _PB, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _sz,
+                                      _vp]),
+    "rc_linear_fp8_backward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32]),
     "rc_status_string": (ctypes.c_char_p, [_i32]),
     "rc_last_error": (ctypes.c_char_p, []),
 }
@@ -537,6 +551,166 @@ def linear(a, w, residual=None, out=None, stream=None):
     _call(lib().rc_linear, dev, stream, M, N, K, a.data_ptr(), lda, w.data_ptr(), _ptr(residual), ldr, out.data_ptr(),
           ldo)
     return out
+
+
+# ---------------------------------------------------------------- projections in 8 bits
+class Fp8Blocks:
+    """A [rows, cols] matrix as e4m3 codes with one power-of-two scale per block
+    of 128 values (rc_blocks8), made by ``quantize_blocks``.
+
+    codes: uint8 [rows, cols rounded up to 128], zeros past the last column;
+    exps: uint8 [blocks of a row, rows rounded up to 16], exponent + 127 of the
+    block of (row, col) at [col // 128, row]; t: the transposed matrix, for
+    weights quantised with ``transposed=True``, else None."""
+
+    __slots__ = ("codes", "exps", "shape", "t", "c")
+
+    def __init__(self, codes, exps, shape, t=None):
+        rows, cols = shape
+        want = (rows, -(-cols // 128) * 128), (-(-cols // 128), -(-rows // 16) * 16)
+        for x, w, what in ((codes, want[0], "codes"), (exps, want[1], "exps")):
+            _expect(x, w, "torch.uint8", what)
+        _same_device(codes.device, exps=exps, t=None if t is None else t.codes)
+        self.codes, self.exps, self.shape, self.t = codes, exps, (rows, cols), t
+        self.c = rc_blocks8(codes.data_ptr(), want[0][1], exps.data_ptr(), want[1][1])
+
+    @staticmethod
+    def empty(rows, cols, device, stream=None, t=None):
+        u8, blocks = _torch().uint8, -(-cols // 128)
+        return Fp8Blocks(_empty((rows, blocks * 128), u8, device, stream),
+                         _empty((blocks, -(-rows // 16) * 16), u8, device, stream), (rows, cols), t)
+
+
+def _blocks(b, what, rows=None, cols=None):
+    if not isinstance(b, Fp8Blocks):
+        raise ValueError(f"{what} must be Fp8Blocks (quantize_blocks makes them), got {type(b).__name__}")
+    if not b.codes.is_cuda:
+        raise ValueError(f"{what} must be on a GPU, got {b.codes.device}")
+    want = (b.shape[0] if rows is None else rows, b.shape[1] if cols is None else cols)
+    if b.shape != want:
+        raise ValueError(f"{what} must be {want}, got {b.shape}")
+    return b
+
+
+def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) -> Fp8Blocks:
+    """x [M, K] bf16 (any row stride) in e4m3 with one power-of-two scale per
+    128 values of a row, or with ``square`` per 128 x 128 values; ``transposed``
+    (square only): with the transposed matrix as ``.t``, which the inputs'
+    gradient of a projection reads.  Weights are quantised once, square; activations per
+    call, and what a projection has read is the checkpoint for its weights' gradient."""
+    ldx = _rows_view(x, "x")
+    dev = x.device
+    M, K = x.shape
+    if transposed and not square:
+        raise ValueError("transposed needs square=True: a block of a row is no block of its transpose")
+    if out is None:
+        out = Fp8Blocks.empty(M, K, dev, stream, Fp8Blocks.empty(K, M, dev, stream) if transposed else None)
+    else:
+        _blocks(out, "out", M, K)
+        if transposed:
+            _blocks(out.t, "out.t", K, M)
+        _same_device(dev, out=out.codes)
+    _call(lib().rc_quantize_blocks, dev, stream, M, K, x.data_ptr(), ldx, int(square), ctypes.byref(out.c),
+          ctypes.byref(out.t.c) if transposed else None)
+    return out
+
+
+def dequantize_blocks(x, out=None, stream=None):
+    """The values of Fp8Blocks in bf16 [M, K] (exact).  Returns out."""
+    M, K = _blocks(x, "x").shape
+    dev = x.codes.device
+    if out is None:
+        out = _empty((M, K), _torch().bfloat16, dev, stream)
+    elif out.shape != (M, K):
+        raise ValueError(f"out must have shape {(M, K)}, got {tuple(out.shape)}")
+    ldo = _rows_view(out, "out")
+    _same_device(dev, out=out)
+    _call(lib().rc_dequantize_blocks, dev, stream, M, K, ctypes.byref(x.c), out.data_ptr(), ldo)
+    return out
+
+
+def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
+    """out = a @ w.T (+ residual) in 8 bits: w [N, K] Fp8Blocks, a [M, K] Fp8Blocks
+    or bf16 (any row stride; quantised per 128 values of a row on the way, into the
+    workspace); bf16 out, fp32 accumulation.  residual, out: [M, N] (any row
+    stride; out may be residual).  A row's result does not depend on M for
+    Fp8Blocks; a bf16 call of up to 16 rows sums in another order.  Returns out."""
+    torch, L = _torch(), lib()
+    blocks = isinstance(a, Fp8Blocks)
+    lda = 0 if blocks else _rows_view(a, "a")
+    M, K = a.shape
+    dev = _blocks(a, "a").codes.device if blocks else a.device
+    N = _blocks(w, "w", cols=K).shape[0]
+    if out is None:
+        out = _empty((M, N), torch.bfloat16, dev, stream)
+    for name, t in (("out", out), ("residual", residual)):
+        if t is not None and t.shape != (M, N):
+            raise ValueError(f"{name} must have shape {(M, N)}, got {tuple(t.shape)}")
+    ldo = _rows_view(out, "out")
+    ldr = _rows_view(residual, "residual") if residual is not None else 0
+    _same_device(dev, w=w.codes, out=out, residual=residual)
+    if blocks:
+        _call(L.rc_linear_fp8_blocks, dev, stream, M, N, K, ctypes.byref(a.c), ctypes.byref(w.c), _ptr(residual), ldr,
+              out.data_ptr(), ldo)
+        return out
+    need = L.rc_linear_fp8_workspace_bytes(M, N, K)
+    workspace = _workspace(workspace, need, dev, stream)
+    _call(L.rc_linear_fp8, dev, stream, M, N, K, a.data_ptr(), lda, ctypes.byref(w.c), _ptr(residual), ldr,
+          out.data_ptr(), ldo, _ptr(workspace), need)
+    return out
+
+
+def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True, want_dw=True, workspace=None,
+                        stream=None):
+    """The gradient of linear_fp8 for dy [M, N] bf16: x [M, K] Fp8Blocks, the input
+    that the product has read; w [N, K] Fp8Blocks with their transposed form.
+    dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row;
+    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual.  Returns (dx, dw), None
+    for what is not wanted (x and w may then be None)."""
+    torch, L = _torch(), lib()
+    lddy = _rows_view(dy, "dy")
+    dev = dy.device
+    M, N = dy.shape
+    if not (want_dx or want_dw):
+        raise ValueError("neither dx nor dw is wanted")
+    if residual is not None and not want_dx:
+        raise ValueError("residual goes with dx")
+    if (dx is not None and not want_dx) or (dw is not None and not want_dw):
+        raise ValueError("dx or dw is given but not wanted")
+    K = (_blocks(w, "w", rows=N) if want_dx else _blocks(x, "x", rows=M)).shape[1]
+    w_t = None
+    if want_dx:
+        if w.t is None:
+            raise ValueError("w has no transposed form: quantize_blocks(w, square=True, transposed=True)")
+        w_t = _blocks(w.t, "w.t", K, N)
+        if dx is None:
+            dx = _empty((M, K), torch.bfloat16, dev, stream)
+        for name, t in (("dx", dx), ("residual", residual)):
+            if t is not None and t.shape != (M, K):
+                raise ValueError(f"{name} must have shape {(M, K)}, got {tuple(t.shape)}")
+    if want_dw:
+        _blocks(x, "x", M, K)
+        if dw is None:
+            dw = _empty((N, K), torch.float32, dev, stream)
+        _expect(dw, (N, K), "torch.float32", "dw")
+    lddx = _rows_view(dx, "dx") if want_dx else 0
+    ldr = _rows_view(residual, "residual") if residual is not None else 0
+    _same_device(dev, dx=dx, dw=dw, residual=residual, x=x.codes if want_dw else None, w=w_t.codes if want_dx else None)
+    need = L.rc_linear_fp8_backward_workspace_bytes(M, N, K, int(want_dx), int(want_dw))
+    workspace = _workspace(workspace, need, dev, stream)
+    _call(L.rc_linear_fp8_backward, dev, stream, M, N, K, dy.data_ptr(), lddy, ctypes.byref(x.c) if want_dw else None,
+          ctypes.byref(w_t.c) if want_dx else None, _ptr(residual), ldr, _ptr(dx), lddx, _ptr(dw), K, _ptr(workspace), need)
+    return dx, dw
+
+
+def _workspace(workspace, need, dev, stream):
+    """The caller's workspace where it is large enough, else one of this call's."""
+    if not need:
+        return None
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        return _empty(need, _torch().uint8, dev, stream, returned=False)
+    _same_device(dev, workspace=workspace)
+    return workspace
 
 
 # ---------------------------------------------------------------- rotation of queries and keys

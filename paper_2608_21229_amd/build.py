@@ -25,7 +25,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librefcache.so")
 SOURCES = ["layout.cpp", "api.cpp", "attn_fwd.hip", "attn_bwd.hip", "linear.hip", "fp8_cache.hip",
-           "rotary.hip", "norm.hip"]
+           "rotary.hip", "norm.hip", "blocks8.hip", "linear8.hip", "wgrad8.hip"]
 # The attention gradient keeps its output accumulators in accumulation registers
 # by its own statements; every other matrix product of it stays in vector ones.
 SOURCE_FLAGS = {"attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}

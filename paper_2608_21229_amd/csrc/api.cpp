@@ -7,6 +7,7 @@
 
 #include <algorithm>
 
+#include "rc_blocks8.h"
 #include "rc_layer.h"
 
 namespace rc {
@@ -1395,6 +1396,263 @@ rc_status rc_gated_norm_backward(const rc_norm* d, const void* dy, int64_t lddy,
   p.partial = static_cast<float*>(workspace);
   RC_TRY(check_launcher(launch_norm_backward, "gated norm gradient"));
   RC_TRY(hip_status(launch_norm_backward(p, stream), "gated norm gradient launch"));
+  return RC_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- projections in 8 bits
+namespace rc {
+namespace {
+
+rc_status check_size8(const char* what, int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || M > kMaxRows8 || N <= 0 || K <= 0) {
+    set_error("%s: %lld rows and columns %lld, %lld must be in [0, 2^28], > 0, > 0", what, (long long)M, (long long)N,
+              (long long)K);
+    return RC_ERR_ARG;
+  }
+  if (N % 8 != 0 || K % 8 != 0 || N > kMaxCols8 || K > kMaxCols8) {
+    set_error("%s: columns %lld, %lld must be multiples of 8 up to 2^22", what, (long long)N, (long long)K);
+    return RC_ERR_UNSUPPORTED;
+  }
+  return RC_OK;
+}
+
+rc_status check_ld8(int64_t ld, int64_t cols, const char* name) {
+  if (ld < cols || ld % 8 != 0 || ld > kMaxCols8) {
+    set_error("row stride %lld of %s must be >= %lld, a multiple of 8, <= 2^22", (long long)ld, name, (long long)cols);
+    return RC_ERR_ARG;
+  }
+  return RC_OK;
+}
+
+rc_status check_blocks8(const rc_blocks8* b, int64_t rows, int64_t cols, const char* name) {
+  if (!b) {
+    set_error("%s is null", name);
+    return RC_ERR_ARG;
+  }
+  RC_TRY(check_ptr(b->codes, name));
+  RC_TRY(check_ptr(b->exps, name));
+  if (b->ld < pad8(cols) || b->ld % 16 != 0 || b->ld > kMaxCols8) {
+    set_error("%s: ld = %lld must be >= %lld, a multiple of 16, <= 2^22", name, (long long)b->ld, (long long)pad8(cols));
+    return RC_ERR_ARG;
+  }
+  if (b->ld_exps < pitch8(rows) || b->ld_exps % 16 != 0 || b->ld_exps > kMaxRows8) {
+    set_error("%s: ld_exps = %lld must be >= %lld, a multiple of 16, <= 2^28", name, (long long)b->ld_exps,
+              (long long)pitch8(rows));
+    return RC_ERR_ARG;
+  }
+  return RC_OK;
+}
+
+Blocks8 blocks_of(const rc_blocks8* b) {
+  return Blocks8{static_cast<uint8_t*>(b->codes), b->ld, static_cast<uint8_t*>(b->exps), b->ld_exps};
+}
+
+// Blocks of [rows, cols] in a workspace: codes, then exponents.
+size_t blocks8_bytes(int64_t rows, int64_t cols) { return size_t(rows * pad8(cols) + blocks8(cols) * pitch8(rows)); }
+
+Blocks8 blocks_in(void* workspace, int64_t rows, int64_t cols) {
+  uint8_t* p = static_cast<uint8_t*>(workspace);
+  return Blocks8{p, pad8(cols), p + rows * pad8(cols), pitch8(rows)};
+}
+
+rc_status check_workspace8(const char* what, const void* workspace, size_t have, size_t need) {
+  if (need > 0 && (!workspace || !aligned16(workspace) || have < need)) {
+    set_error("%s needs a 16-byte aligned workspace of %zu bytes (got %zu)", what, need, workspace ? have : size_t(0));
+    return RC_ERR_WORKSPACE;
+  }
+  return RC_OK;
+}
+
+// Work-groups of the largest launch over [M, N] outputs and [M, K] rows.
+rc_status check_grid8(int64_t M, int64_t N, int64_t K, const char* what) {
+  RC_TRY(check_blocks((M + 63) / 64 * ((N + 63) / 64), what));
+  return check_blocks((M + 31) / 32 * ((blocks8(K) + 3) / 4), what);
+}
+
+rc_status run_linear8(int64_t M, int32_t N, int32_t K, Linear8Params& q, const void* r, int64_t ldr, void* out,
+                      int64_t ldo, void* workspace, void* stream) {
+  q.r = static_cast<const uint16_t*>(r);
+  q.ldr = r ? ldr : 0;
+  q.out = static_cast<uint16_t*>(out);
+  q.ldo = ldo;
+  q.M = M;
+  q.N = N;
+  q.K = K;
+  if (q.x && M <= kFewRows8) return hip_status(launch_linear8_few(q, stream), "FP8 linear launch");
+  if (q.x) {
+    q.a = blocks_in(workspace, M, K);
+    const Quant8Params z{q.x, q.ldx, M, K, q.a, Blocks8{nullptr, 0, nullptr, 0}};
+    RC_TRY(hip_status(launch_quantize_rows(z, stream), "block quantisation launch"));
+  }
+  return hip_status(launch_linear8(q, plan_linear8(M, N, K), stream), "FP8 linear launch");
+}
+
+// The arguments of a product's output and residual.
+rc_status check_out8(int64_t N, const void* r, int64_t ldr, const void* out, int64_t ldo) {
+  RC_TRY(check_ptr(out, "out"));
+  RC_TRY(check_ld8(ldo, N, "out"));
+  if (r) {
+    RC_TRY(check_ptr(r, "r"));
+    RC_TRY(check_ld8(ldr, N, "r"));
+  }
+  return RC_OK;
+}
+
+size_t linear8_workspace(int64_t M, int64_t K) { return M <= kFewRows8 ? 0 : blocks8_bytes(M, K); }
+
+size_t wgrad8_partial_bytes(int64_t M, int32_t N, int32_t K) {
+  const int32_t splits = plan_wgrad8(M, N, K).splits;
+  return splits > 1 ? size_t(splits) * N * K * sizeof(float) : 0;
+}
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+}  // namespace
+}  // namespace rc
+
+extern "C" {
+
+rc_status rc_quantize_blocks(int64_t M, int32_t K, const void* x, int64_t ldx, int32_t square, const rc_blocks8* out,
+                             const rc_blocks8* out_t, void* stream) {
+  using namespace rc;
+  RC_TRY(check_size8("block quantisation", M, 8, K));
+  if (out_t && !square) {
+    set_error("block quantisation: only squares have a transposed form");
+    return RC_ERR_UNSUPPORTED;
+  }
+  if (M == 0) return RC_OK;
+  RC_TRY(check_ptr(x, "x"));
+  RC_TRY(check_ld8(ldx, K, "x"));
+  RC_TRY(check_blocks8(out, M, K, "out"));
+  if (out_t) {
+    RC_TRY(check_size8("block quantisation, transposed", K, M, 8));
+    RC_TRY(check_blocks8(out_t, K, M, "out_t"));
+  }
+  RC_TRY(check_grid8(M, 8, K, "block quantisation"));
+  RC_TRY(check_launcher(launch_quantize_rows, "block quantisation"));
+  const Quant8Params q{static_cast<const uint16_t*>(x), ldx, M, K, blocks_of(out),
+                       out_t ? blocks_of(out_t) : Blocks8{nullptr, 0, nullptr, 0}};
+  return hip_status((square ? launch_quantize_squares : launch_quantize_rows)(q, stream), "block quantisation launch");
+}
+
+rc_status rc_dequantize_blocks(int64_t M, int32_t K, const rc_blocks8* x, void* out, int64_t ldo, void* stream) {
+  using namespace rc;
+  RC_TRY(check_size8("block expansion", M, 8, K));
+  if (M == 0) return RC_OK;
+  RC_TRY(check_blocks8(x, M, K, "x"));
+  RC_TRY(check_ptr(out, "out"));
+  RC_TRY(check_ld8(ldo, K, "out"));
+  RC_TRY(check_blocks((M * (K / 8) + 255) / 256, "block expansion"));
+  RC_TRY(check_launcher(launch_dequantize, "block expansion"));
+  const Dequant8Params q{blocks_of(x), M, K, static_cast<uint16_t*>(out), ldo};
+  return hip_status(launch_dequantize(q, stream), "block expansion launch");
+}
+
+rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8* a, const rc_blocks8* w,
+                               const void* r, int64_t ldr, void* out, int64_t ldo, void* stream) {
+  using namespace rc;
+  RC_TRY(check_size8("FP8 linear", M, N, K));
+  if (M == 0) return RC_OK;
+  RC_TRY(check_blocks8(a, M, K, "a"));
+  RC_TRY(check_blocks8(w, N, K, "w"));
+  RC_TRY(check_out8(N, r, ldr, out, ldo));
+  RC_TRY(check_grid8(M, N, K, "FP8 linear"));
+  RC_TRY(check_launcher(launch_linear8, "FP8 linear"));
+  Linear8Params q{};
+  q.a = blocks_of(a);
+  q.w = blocks_of(w);
+  return run_linear8(M, N, K, q, r, ldr, out, ldo, nullptr, stream);
+}
+
+size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+  using namespace rc;
+  return check_size8("FP8 linear", M, N, K) == RC_OK ? linear8_workspace(M, K) : 0;
+}
+
+rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const rc_blocks8* w,
+                        const void* r, int64_t ldr, void* out, int64_t ldo, void* workspace, size_t ws_bytes,
+                        void* stream) {
+  using namespace rc;
+  RC_TRY(check_size8("FP8 linear", M, N, K));
+  if (M == 0) return RC_OK;
+  RC_TRY(check_ptr(a, "a"));
+  RC_TRY(check_ld8(lda, K, "a"));
+  RC_TRY(check_blocks8(w, N, K, "w"));
+  RC_TRY(check_out8(N, r, ldr, out, ldo));
+  RC_TRY(check_grid8(M, N, K, "FP8 linear"));
+  RC_TRY(check_workspace8("FP8 linear", workspace, ws_bytes, linear8_workspace(M, K)));
+  RC_TRY(check_launcher(launch_linear8, "FP8 linear"));
+  Linear8Params q{};
+  q.x = static_cast<const uint16_t*>(a);
+  q.ldx = lda;
+  q.w = blocks_of(w);
+  return run_linear8(M, N, K, q, r, ldr, out, ldo, workspace, stream);
+}
+
+size_t rc_linear_fp8_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t want_dx, int32_t want_dw) {
+  using namespace rc;
+  if (check_size8("FP8 linear's gradient", M, N, K) != RC_OK) return 0;
+  return (want_dx ? round16(linear8_workspace(M, N)) : 0) + (want_dw ? wgrad8_partial_bytes(M, N, K) : 0);
+}
+
+rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy, int64_t lddy, const rc_blocks8* x,
+                                 const rc_blocks8* w_t, const void* r, int64_t ldr, void* dx, int64_t lddx, float* dw,
+                                 int64_t lddw, void* workspace, size_t ws_bytes, void* stream) {
+  using namespace rc;
+  RC_TRY(check_size8("FP8 linear's gradient", M, N, K));
+  // of no rows dx has no memory; dw are zeros
+  if (M > 0 && !dx && !dw) {
+    set_error("FP8 linear's gradient: neither dx nor dw is wanted");
+    return RC_ERR_ARG;
+  }
+  if (M > 0 && ((!dx && (w_t || r)) || (!dw && x))) {
+    set_error("FP8 linear's gradient: w_t and r go with dx, x with dw");
+    return RC_ERR_ARG;
+  }
+  if (M > 0) {
+    RC_TRY(check_ptr(dy, "dy"));
+    RC_TRY(check_ld8(lddy, N, "dy"));
+  }
+  if (dx && M > 0) {
+    RC_TRY(check_blocks8(w_t, K, N, "w_t"));
+    RC_TRY(check_out8(K, r, ldr, dx, lddx));
+    RC_TRY(check_grid8(M, K, N, "FP8 linear's gradient"));
+  }
+  if (dw) {
+    RC_TRY(check_ptr(dw, "dw"));
+    RC_TRY(check_ld8(lddw, K, "dw"));
+    if (M > 0) RC_TRY(check_blocks8(x, M, K, "x"));
+    RC_TRY(check_blocks((int64_t(N) + 127) / 128 * ((K + 127) / 128) * plan_wgrad8(M, N, K).splits, "FP8 weights' gradient"));
+    RC_TRY(check_blocks((int64_t(N) * (K / 4) + 255) / 256, "FP8 weights' gradient"));
+  }
+  RC_TRY(check_workspace8("FP8 linear's gradient", workspace, ws_bytes,
+                          rc_linear_fp8_backward_workspace_bytes(M, N, K, dx != nullptr, dw != nullptr)));
+  RC_TRY(check_launcher(launch_linear8, "FP8 linear's gradient"));
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (dx && M > 0) {
+    Linear8Params q{};
+    q.x = static_cast<const uint16_t*>(dy);
+    q.ldx = lddy;
+    q.w = blocks_of(w_t);
+    RC_TRY(run_linear8(M, K, N, q, r, ldr, dx, lddx, ws, stream));
+  }
+  if (dw) {
+    const WGrad8Plan plan = plan_wgrad8(M, N, K);
+    WGrad8Params q{};
+    q.dy = static_cast<const uint16_t*>(dy);
+    q.lddy = lddy;
+    if (M > 0) q.x = blocks_of(x);
+    q.dw = dw;
+    q.lddw = lddw;
+    q.partial = reinterpret_cast<float*>(ws + (dx ? round16(linear8_workspace(M, N)) : 0));
+    q.M = M;
+    q.N = N;
+    q.K = K;
+    q.splits = plan.splits;
+    RC_TRY(hip_status(launch_wgrad8(q, plan.tile, stream), "FP8 weights' gradient launch"));
+  }
   return RC_OK;
 }
 

@@ -1,0 +1,141 @@
+// Quantisation to e4m3 codes with one power-of-two scale per block of 128
+// values, and back.
+//
+// A block's scale is 2^e with the smallest e >= -127 that brings its largest
+// finite magnitude to at most 448, the largest e4m3 value; e = 0 for a block of
+// zeros.  The code of x is the e4m3 value nearest to x 2^-e (ties to even):
+// multiplying by a power of two is exact, so a code depends on its value and
+// the block's maximum alone.  Infinities and NaN become the code of NaN.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "rc_blocks8.h"
+#include "rc_device.h"
+#include "rc_quant8.h"
+
+namespace rc {
+namespace {
+
+// Blocks of a row.  A work-group takes kRows rows of four blocks: 16 lanes hold
+// a block, 8 values each, so a wave reads 1 KB of a row at once, and all of a
+// thread's rows are in flight together.  The exponents are gathered in LDS so
+// that a block's column of them is written in runs of kRows bytes.
+// Memory-bound: 2 bytes read and 1 written per value.
+constexpr int kRows = 32;
+
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const Quant8Params q) {
+  __shared__ uint8_t exps[4][kRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int kblocks = (q.K + kBlock8 - 1) / kBlock8, groups = (kblocks + 3) / 4;
+  const int64_t m0 = int64_t(blockIdx.x) / groups * kRows;
+  const int kb0 = int(blockIdx.x % groups) * 4;
+  const int kb = kb0 + (lane >> 4);
+  const int64_t col = int64_t(kb0) * kBlock8 + lane * 8;
+  u32x4 v[kRows / 4];
+#pragma unroll
+  for (int i = 0; i < kRows / 4; ++i) {
+    const int64_t m = m0 + i * 4 + wave;
+    v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (m < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + col);
+  }
+#pragma unroll
+  for (int i = 0; i < kRows / 4; ++i) {
+    const int row = i * 4 + wave;
+    const uint32_t byte = exponent_byte(group_max16(finite_amax8(v[i])));
+    if (m0 + row < q.M && kb < kblocks) *reinterpret_cast<u32x2*>(q.out.codes + (m0 + row) * q.out.ld + col) = codes8(v[i], byte);
+    if ((lane & 15) == 0) exps[lane >> 4][row] = uint8_t(byte);
+  }
+  __syncthreads();
+  if (threadIdx.x < 4 * kRows / 4) {
+    const int k = threadIdx.x / (kRows / 4), r = threadIdx.x % (kRows / 4) * 4;
+    if (kb0 + k < kblocks && m0 + r < q.out.le)
+      *reinterpret_cast<uint32_t*>(q.out.exps + int64_t(kb0 + k) * q.out.le + m0 + r) =
+          *reinterpret_cast<const uint32_t*>(&exps[k][r]);
+  }
+}
+
+// Squares of 128 x 128, one per work-group; the transposed codes go through
+// LDS.  Rows and columns up to the next multiple of 128 exist as zeros.
+__global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Params q) {
+  constexpr int kPitch = kBlock8 + 8;
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kPitch];
+  __shared__ float red[4];
+  const int t = threadIdx.x;
+  const int kblocks = (q.K + kBlock8 - 1) / kBlock8;
+  const int64_t nb = int64_t(blockIdx.x) / kblocks;
+  const int kb = int(blockIdx.x % kblocks);
+  const int64_t m0 = nb * kBlock8, k0 = int64_t(kb) * kBlock8;
+  const int64_t col = k0 + (t & 15) * 8;
+  u32x4 v[8];
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t m = m0 + i * 16 + (t >> 4);
+    v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (m < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + col);
+    a = fmaxf(a, finite_amax8(v[i]));
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
+  if ((t & 63) == 0) red[t >> 6] = a;
+  __syncthreads();
+  const uint32_t byte = exponent_byte(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = i * 16 + (t >> 4);
+    const u32x2 c = codes8(v[i], byte);
+    if (m0 + row < q.M) *reinterpret_cast<u32x2*>(q.out.codes + (m0 + row) * q.out.ld + col) = c;
+    if (q.out_t.codes) *reinterpret_cast<u32x2*>(tile + row * kPitch + (t & 15) * 8) = c;
+  }
+  const uint32_t four = byte * 0x01010101u;
+  if (t < 32) {
+    if (m0 + t * 4 < q.out.le) *reinterpret_cast<uint32_t*>(q.out.exps + kb * q.out.le + m0 + t * 4) = four;
+  } else if (t < 64 && q.out_t.codes) {
+    const int r = (t - 32) * 4;
+    if (k0 + r < q.out_t.le) *reinterpret_cast<uint32_t*>(q.out_t.exps + nb * q.out_t.le + k0 + r) = four;
+  }
+  if (!q.out_t.codes) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int k = i * 16 + (t >> 4), n = (t & 15) * 8;
+    u32x2 c{0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e / 4] |= uint32_t(tile[(n + e) * kPitch + k]) << (8 * (e & 3));
+    if (k0 + k < q.K) *reinterpret_cast<u32x2*>(q.out_t.codes + (k0 + k) * q.out_t.ld + m0 + n) = c;
+  }
+}
+
+// 8 codes per thread back to bf16, exact (4 significant bits) above bf16's smallest.
+__global__ __launch_bounds__(256) void dequantize_kernel(const Dequant8Params q) {
+  const int g = q.K / 8;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= q.M * g) return;
+  const int64_t m = i / g;
+  const int col = int(i % g) * 8;
+  const u32x2 c = *reinterpret_cast<const u32x2*>(q.x.codes + m * q.x.ld + col);
+  *reinterpret_cast<u32x4*>(q.out + m * q.ldo + col) = values8(c, q.x.exps[int64_t(col / kBlock8) * q.x.le + m]);
+}
+
+}  // namespace
+
+int launch_quantize_rows(const Quant8Params& q, void* stream) {
+  const int64_t groups = (blocks8(q.K) + 3) / 4;
+  hipLaunchKernelGGL(quantize_rows_kernel, dim3((q.M + kRows - 1) / kRows * groups), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), q);
+  return int(hipGetLastError());
+}
+
+int launch_quantize_squares(const Quant8Params& q, void* stream) {
+  hipLaunchKernelGGL(quantize_squares_kernel, dim3(blocks8(q.M) * blocks8(q.K)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), q);
+  return int(hipGetLastError());
+}
+
+int launch_dequantize(const Dequant8Params& q, void* stream) {
+  hipLaunchKernelGGL(dequantize_kernel, dim3((q.M * (q.K / 8) + 255) / 256), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), q);
+  return int(hipGetLastError());
+}
+
+}  // namespace rc

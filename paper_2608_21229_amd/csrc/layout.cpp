@@ -15,6 +15,7 @@
 #include <queue>
 #include <vector>
 
+#include "rc_blocks8.h"
 #include "rc_internal.h"
 
 namespace rc {
@@ -496,6 +497,39 @@ LinearPlan plan_linear(const LinearParams& q) {
         }
   }
   p.tile = pick_linear(q);
+  return p;
+}
+
+// The tile of an FP8 product: as pick_linear, a slice being 128 codes.
+int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
+  struct {
+    int64_t fixed, slice;
+  } constexpr kCost[] = {{5500, 1475}, {3700, 806}, {3200, 473}, {2500, 380}, {1800, 223}};
+  int32_t best = 0;
+  int64_t best_cost = INT64_MAX;
+  for (int32_t i = 0; i < 5; ++i) {
+    const Tile8& t = kLinear8Tiles[i];
+    const int64_t tiles = (M + t.bm - 1) / t.bm * ((N + t.bn - 1) / t.bn);
+    const int64_t cost = (tiles + kCUs - 1) / kCUs * (kCost[i].fixed + kCost[i].slice * blocks8(K));
+    if (cost < best_cost) {
+      best = i;
+      best_cost = cost;
+    }
+  }
+  return best;
+}
+
+// The tile of a weights' gradient, and the shares of the rows where the tiles
+// alone leave CUs idle.
+WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K) {
+  WGrad8Plan p{0, 1};
+  const auto tiles = [&](int32_t i) {
+    const Tile8& t = kWGrad8Tiles[i];
+    return int64_t((N + t.bm - 1) / t.bm) * ((K + t.bn - 1) / t.bn);
+  };
+  if (tiles(0) < kCUs / 2) p.tile = 1;
+  const int64_t slices = (M + 63) / 64, n = tiles(p.tile);
+  if (n < kCUs) p.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(kCUs / n, slices / 4)));
   return p;
 }
 

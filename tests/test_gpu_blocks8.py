@@ -1,0 +1,300 @@
+"""Projections in 8 bits on the GPU against their definition in 64 bits."""
+import pytest
+import torch
+
+import paper_2608_21229_amd as rc
+from tests import blocks8_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(1, 8), (1, 128), (3, 136), (16, 64), (31, 1024), (33, 1032), (128, 520), (257, 2560), (1000, 264)]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def near(got, want, magnitude, adds, rounding, cut=0.0):
+    """|got - want| within the last rounding, the sums' (`adds` of them, each off
+    by at most 2^-23 of the magnitudes summed so far) and the products' (cut)."""
+    got, want = got.cpu().double(), want.double()
+    assert got.shape == want.shape
+    tol = rounding * want.abs() + (adds * 2.0 ** -23 * magnitude + cut) * (1 + rounding) + 2.0 ** -134
+    off = (got - want).abs()
+    print(f"[blocks8] err/bound={float((off / tol).max()):.3f}", flush=True)
+    assert bool((off <= tol).all()), float((off - tol).max())
+
+
+def product(a, w):
+    """a w^T of block values (fp64), the sum of its magnitudes, and how far the 8-bit
+    matrix instruction may be off.  It sums 64 or 128 products to the accumulator
+    after cutting each, towards zero, below 2^-13 of the product of the powers of two in
+    the operands' largest magnitudes.  A block's 128 cuts are below q = 2^-13 max|a| max|w| each
+    and have the signs of their products, which are random here: their sum has a deviation of at
+    most q sqrt(128 / 3) per block, and 8 deviations are allowed (for a single block also more than
+    the certain 8 to 50 q of that many products)."""
+    def top(v):
+        v = torch.nn.functional.pad(v.abs(), (0, -v.shape[1] % 128))
+        return v.unflatten(1, (-1, 128)).amax(2).square()
+    cut = 8 * 2.0 ** -13 * (128 / 3 * (top(a) @ top(w).t())).sqrt()
+    return a @ w.t(), a.abs() @ w.t().abs(), cut
+
+
+def adds8(k):
+    return k / 64 + 64 + 8  # instructions, values in one, shares joined
+
+
+@pytest.mark.parametrize("m,k", SIZES)
+@pytest.mark.parametrize("wide", [0, 24])
+def test_quantize_rows(m, k, wide):
+    x = plain.rows(gen(m + k), m, k, wide=wide)
+    b = rc.quantize_blocks(x)
+    codes, exps, values = plain.quantize(x)
+    assert torch.equal(plain.codes_of(b), codes) and torch.equal(plain.exps_of(b), exps)
+    assert not b.codes[:, k:].any()
+    assert torch.equal(rc.dequantize_blocks(b).cpu().double(), values)
+
+
+@pytest.mark.parametrize("n,k", [(8, 8), (128, 128), (136, 8), (8, 136), (384, 128), (520, 1032), (1000, 264)])
+def test_quantize_squares(n, k):
+    x = plain.rows(gen(n * k), n, k, wide=8)
+    b = rc.quantize_blocks(x, square=True, transposed=True)
+    codes, exps, values = plain.quantize(x, square=True)
+    assert torch.equal(plain.codes_of(b), codes) and torch.equal(plain.exps_of(b, True), exps)
+    assert torch.equal(plain.codes_of(b.t), codes.t()) and torch.equal(plain.exps_of(b.t, True), exps.t())
+    assert not b.codes[:, k:].any() and not b.t.codes[:, n:].any()
+    assert torch.equal(rc.dequantize_blocks(b).cpu().double(), values)
+    assert torch.equal(rc.dequantize_blocks(b.t).cpu().double(), values.t())
+    again = rc.quantize_blocks(x, square=True)
+    assert again.t is None and torch.equal(again.codes, b.codes)
+
+
+def test_quantize_extremes():
+    """Largest, smallest, zero and non-finite values; every border of the grid."""
+    x = torch.zeros(12, 128)
+    x[1, 5] = 2.0 ** -133          # bf16's smallest: the exponent ends at -127
+    x[2, :] = torch.linspace(-448, 448, 128)
+    x[3, 0], x[3, 1] = 3.3e38, 2.0 ** -133
+    x[4, 0], x[4, 1] = float("inf"), 2.0
+    x[5, 0], x[5, 1] = float("nan"), -3.0
+    x[6, :] = float("-inf")
+    x[7, 0], x[7, 1] = 449.0, 1.0
+    x[8, 0], x[8, 1:65] = 256.0, torch.arange(64) / 8 + 1 / 16   # ties between neighbours
+    x[9, 0], x[9, 1:65] = 256.0, torch.arange(64) * 2.0 ** -10   # subnormal codes
+    x[10, :] = 2.0 ** -120
+    x[11, 0], x[11, 1] = 448.0, 464.0
+    x = x.bfloat16().cuda()
+    b = rc.quantize_blocks(x)
+    codes, exps, _ = plain.quantize(x)
+    assert torch.equal(plain.exps_of(b), exps)
+    assert torch.equal(plain.codes_of(b).nan_to_num(999.0), codes.nan_to_num(999.0))
+    back = rc.dequantize_blocks(b).cpu()
+    assert back[4, 0].isnan() and back[5, 0].isnan() and back[6].isnan().all()
+    assert back[4, 1] == 2.0 and back[5, 1] == -3.0 and back[1, 5] == 2.0 ** -133
+
+
+LINEAR = [(1, 8, 8), (1, 128, 128), (2, 2560, 1032), (16, 72, 640), (17, 384, 128), (80, 384, 128), (65, 264, 520),
+          (128, 128, 2560), (129, 1032, 1160), (300, 2568, 264), (1025, 640, 1288)]
+
+
+@pytest.mark.parametrize("m,n,k", LINEAR)
+@pytest.mark.parametrize("residual", [False, True])
+def test_linear(m, n, k, residual):
+    g = gen(m * n + k)
+    x, w = plain.rows(g, m, k, wide=16), plain.rows(g, n, k)
+    r = plain.rows(g, m, n, wide=8) if residual else None
+    w8, x8 = rc.quantize_blocks(w, square=True), rc.quantize_blocks(x)
+    xv, wv = plain.quantize(x)[2], plain.quantize(w, square=True)[2]
+    want, size, cut = product(xv, wv)
+    if residual:
+        want, size = want + r.cpu().double(), size + r.cpu().double().abs()
+    for a in (x, x8):
+        near(rc.linear_fp8(a, w8, residual=r), want, size, adds8(k), 2.0 ** -8, cut)
+
+
+def test_linear_row_blocks_on_both_sides():
+    g = gen(5)
+    x, w = plain.rows(g, 100, 520), plain.rows(g, 200, 520)
+    xv, wv = plain.quantize(x)[2], plain.quantize(w)[2]
+    want, size, cut = product(xv, wv)
+    near(rc.linear_fp8(x, rc.quantize_blocks(w)), want, size, adds8(520), 2.0 ** -8, cut)
+
+
+# one of every tile size, by rounds of 256 work-groups
+@pytest.mark.parametrize("m,n,k", [(4096, 4096, 256), (4096, 2048, 384), (2000, 2048, 256), (900, 2048, 128)])
+def test_linear_tiles(m, n, k):
+    g = torch.Generator(device="cuda").manual_seed(m)
+    x = torch.randn(m, k, generator=g, device="cuda").bfloat16()
+    w = torch.randn(n, k, generator=g, device="cuda").bfloat16()
+    x8, w8 = rc.quantize_blocks(x), rc.quantize_blocks(w, square=True)
+    xv, wv = rc.dequantize_blocks(x8).double(), rc.dequantize_blocks(w8).double()
+    want, size, cut = (t.cpu() for t in product(xv, wv))
+    near(rc.linear_fp8(x, w8), want, size, adds8(k), 2.0 ** -8, cut)
+
+
+def test_linear_rows_do_not_depend_on_each_other():
+    """A row's bits are the same in every call of blocks, whatever tile holds it."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(5000, 1032, generator=g, device="cuda").bfloat16()
+    w8 = rc.quantize_blocks(torch.randn(2568, 1032, generator=g, device="cuda").bfloat16(), square=True)
+    whole = rc.linear_fp8(rc.quantize_blocks(x), w8)
+    for at, n in ((0, 1), (7, 40), (100, 700), (3000, 2000)):
+        assert torch.equal(rc.linear_fp8(rc.quantize_blocks(x[at:at + n]), w8), whole[at:at + n])
+        if n > 16:
+            assert torch.equal(rc.linear_fp8(x[at:at + n], w8), whole[at:at + n])
+
+
+def test_linear_in_place_and_bounds():
+    """out may be the residual; what surrounds a strided output stays."""
+    g = gen(9)
+    x, w8 = plain.rows(g, 70, 136), rc.quantize_blocks(plain.rows(g, 200, 136), square=True)
+    for m in (70, 5):
+        buf = plain.rows(g, m + 2, 200 + 32)
+        keep, out = buf.clone(), buf[1:m + 1, 16:216]
+        want = rc.linear_fp8(x[:m], w8, residual=out.clone())
+        assert rc.linear_fp8(x[:m], w8, residual=out, out=out) is out
+        assert torch.equal(out, want)
+        buf[1:m + 1, 16:216] = keep[1:m + 1, 16:216]
+        assert torch.equal(buf, keep)
+
+
+def test_linear_non_finite_rows():
+    """A row with an infinity or a NaN is NaN, and no other row is."""
+    g = gen(11)
+    w8 = rc.quantize_blocks(plain.rows(g, 136, 264), square=True)
+    for m in (6, 60):
+        x = plain.rows(g, m, 264)
+        want = rc.linear_fp8(x, w8)
+        x[1, 3], x[4, 260] = float("inf"), float("nan")
+        got = rc.linear_fp8(x, w8)
+        bad = torch.zeros(m, dtype=torch.bool, device="cuda")
+        bad[[1, 4]] = True
+        assert got[bad].isnan().all() and torch.equal(got[~bad], want[~bad])
+
+
+def test_linear_extreme_scales():
+    """Blocks near both ends of the exponents multiply to ordinary numbers."""
+    g = gen(12)
+    x = torch.randn(40, 256, generator=g) * torch.tensor([2.0 ** 100, 2.0 ** -100]).repeat_interleave(128)
+    w = torch.randn(128, 256, generator=g) * torch.tensor([2.0 ** -100, 2.0 ** 100]).repeat_interleave(128)
+    x, w = x.bfloat16().cuda(), w.bfloat16().cuda()
+    xv, wv = plain.quantize(x)[2], plain.quantize(w, square=True)[2]
+    want, size, cut = product(xv, wv)
+    for m in (3, 40):
+        near(rc.linear_fp8(x[:m], rc.quantize_blocks(w, square=True)), want[:m], size[:m], adds8(256), 2.0 ** -8, cut[:m])
+
+
+BACKWARD = [(1, 8, 8), (1, 128, 128), (5, 264, 136), (63, 136, 264), (64, 128, 128), (65, 384, 128), (80, 384, 128),
+            (300, 520, 1032), (1000, 264, 72), (5000, 136, 128)]
+
+
+@pytest.mark.parametrize("m,n,k", BACKWARD)
+def test_backward(m, n, k):
+    g = gen(m + n * k)
+    x8 = rc.quantize_blocks(plain.rows(g, m, k))
+    w8 = rc.quantize_blocks(plain.rows(g, n, k), square=True, transposed=True)
+    dy, r = plain.rows(g, m, n, wide=8), plain.rows(g, m, k, wide=16)
+    xv, wv = rc.dequantize_blocks(x8).cpu().double(), rc.dequantize_blocks(w8).cpu().double()
+    dv, dyv = plain.quantize(dy)[2], dy.cpu().double()
+    dx, dw = rc.linear_fp8_backward(dy, x8, w8)
+    want, size, cut = product(dv, wv.t())
+    near(dx, want, size, adds8(n), 2.0 ** -8, cut)
+    near(dw, dyv.t() @ xv, dyv.t().abs() @ xv.abs(), m / 16 + 16 + 64, 2.0 ** -24)
+    only, none = rc.linear_fp8_backward(dy, None, w8, residual=r, want_dw=False)
+    assert none is None
+    near(only, want + r.cpu().double(), size + r.cpu().double().abs(), adds8(n), 2.0 ** -8, cut)
+    none, again = rc.linear_fp8_backward(dy, x8, None, want_dx=False)
+    assert none is None and torch.equal(again, dw)
+
+
+@pytest.mark.parametrize("m,n,k", [(3000, 4096, 4096), (3000, 2568, 1928)])
+def test_weight_gradient_tiles(m, n, k):
+    g = torch.Generator(device="cuda").manual_seed(m + k)
+    x8 = rc.quantize_blocks(torch.randn(m, k, generator=g, device="cuda").bfloat16())
+    dy = torch.randn(m, n, generator=g, device="cuda").bfloat16()
+    xv = rc.dequantize_blocks(x8).double()
+    _, dw = rc.linear_fp8_backward(dy, x8, None, want_dx=False)
+    near(dw, (dy.double().t() @ xv).cpu(), (dy.double().t().abs() @ xv.abs()).cpu(), m / 16 + 16 + 64, 2.0 ** -24)
+    assert torch.equal(dw, rc.linear_fp8_backward(dy, x8, None, want_dx=False)[1])
+
+
+def test_backward_rows_past_the_last():
+    """What the exponents hold past the last row reaches nothing."""
+    g = gen(21)
+    x8 = rc.quantize_blocks(plain.rows(g, 70, 264))
+    dy = plain.rows(g, 70, 136)
+    _, want = rc.linear_fp8_backward(dy, x8, None, want_dx=False)
+    w8 = rc.quantize_blocks(plain.rows(g, 136, 264), square=True)
+    out = rc.linear_fp8(x8, w8)
+    x8.exps[:, 70:] = 255
+    w8.exps[:, 136:] = 255
+    assert torch.equal(rc.linear_fp8_backward(dy, x8, None, want_dx=False)[1], want)
+    assert torch.equal(rc.linear_fp8(x8, w8), out)
+
+
+def test_no_rows():
+    g = gen(22)
+    w8 = rc.quantize_blocks(plain.rows(g, 136, 264), square=True, transposed=True)
+    x = torch.empty(0, 264, dtype=torch.bfloat16, device="cuda")
+    x8 = rc.quantize_blocks(x)
+    assert rc.dequantize_blocks(x8).shape == (0, 264)
+    assert rc.linear_fp8(x, w8).shape == (0, 136) and rc.linear_fp8(x8, w8).shape == (0, 136)
+    dw = torch.full((136, 264), 7.0, device="cuda")
+    dx, got = rc.linear_fp8_backward(torch.empty(0, 136, dtype=torch.bfloat16, device="cuda"), x8, w8, dw=dw)
+    assert dx.shape == (0, 264) and got is dw and not dw.any()
+
+
+def test_gradient_against_differences():
+    """dw and dx are the derivatives of the product of the values: its change along a direction."""
+    g = gen(31)
+    m, n, k = 96, 128, 128
+    w8 = rc.quantize_blocks(plain.rows(g, n, k), square=True, transposed=True)
+    x8 = rc.quantize_blocks(plain.rows(g, m, k))
+    xv, wv = (rc.dequantize_blocks(b).cpu().double() for b in (x8, w8))
+    # one code per row block, so that dy is what its quantisation makes of it
+    dy = (torch.randint(-8, 9, (m, n), generator=g) / 8).bfloat16().cuda()
+    dx, dw = (t.cpu().double() for t in rc.linear_fp8_backward(dy, x8, w8))
+    f = lambda a, b: float(((a @ b.t()) * dy.cpu().double()).sum())  # noqa: E731
+    for _ in range(3):
+        u, v = torch.randn(m, k, generator=g).double(), torch.randn(n, k, generator=g).double()
+        by = (f(xv + u, wv) - f(xv - u, wv)) / 2   # linear in each argument
+        _, size, cut = product(dy.cpu().double(), wv.t())
+        tol = float((u.abs() * ((2.0 ** -8 + adds8(n) * 2.0 ** -23) * size + cut)).sum())
+        assert abs(by - float((u * dx).sum())) <= tol
+        by = (f(xv, wv + v) - f(xv, wv - v)) / 2
+        tol = (2.0 ** -24 + (m / 16 + 80) * 2.0 ** -23) * float((v.abs() * (dy.cpu().double().abs().t() @ xv.abs())).sum())
+        assert abs(by - float((v * dw).sum())) <= tol
+
+
+def test_training_step_on_a_stream_and_captured():
+    """Quantise, product, gradient and expansion together: on a stream of their own, and
+    captured and replayed with eager work between."""
+    g = gen(41)
+    x, w = plain.rows(g, 200, 264), plain.rows(g, 392, 264)
+    dy, r = plain.rows(g, 200, 392), plain.rows(g, 200, 392)
+
+    def step(stream=None):
+        w8 = rc.quantize_blocks(w, square=True, transposed=True, stream=stream)
+        x8 = rc.quantize_blocks(x, stream=stream)
+        out = rc.linear_fp8(x8, w8, residual=r, stream=stream)
+        few = rc.linear_fp8(x[:9], w8, stream=stream)
+        dx, dw = rc.linear_fp8_backward(dy, x8, w8, stream=stream)
+        return out, few, dx, dw, rc.dequantize_blocks(x8, stream=stream)
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(3):
+        x.copy_(plain.rows(gen(50 + i), 200, 264))
+        dy.mul_(0.5)
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
