@@ -563,33 +563,42 @@ class Fp8Blocks:
     block of (row, col) at [col // 128, row]; t: the transposed matrix, for
     weights quantised with ``transposed=True``, else None."""
 
-    __slots__ = ("codes", "exps", "shape", "t", "c")
+    __slots__ = ("codes", "exps", "shape", "t", "c", "device")
 
     def __init__(self, codes, exps, shape, t=None):
         rows, cols = shape
         want = (rows, -(-cols // 128) * 128), (-(-cols // 128), -(-rows // 16) * 16)
         for x, w, what in ((codes, want[0], "codes"), (exps, want[1], "exps")):
             _expect(x, w, "torch.uint8", what)
-        _same_device(codes.device, exps=exps, t=None if t is None else t.codes)
-        self.codes, self.exps, self.shape, self.t = codes, exps, (rows, cols), t
-        self.c = rc_blocks8(codes.data_ptr(), want[0][1], exps.data_ptr(), want[1][1])
+        _same_device(codes.device, exps=exps, t=t)
+        if t is not None and t.shape != (cols, rows):
+            raise ValueError(f"t must be {(cols, rows)}, got {t.shape}")
+        self._set(codes, exps, (rows, cols), t)
+
+    def _set(self, codes, exps, shape, t):
+        self.codes, self.exps, self.shape, self.t, self.device = codes, exps, shape, t, codes.device
+        self.c = rc_blocks8(codes.data_ptr(), -(-shape[1] // 128) * 128, exps.data_ptr(), -(-shape[0] // 16) * 16)
 
     @staticmethod
     def empty(rows, cols, device, stream=None, t=None):
+        """Memory for [rows, cols] (of stream's, as a call's own outputs)."""
         u8, blocks = _torch().uint8, -(-cols // 128)
-        return Fp8Blocks(_empty((rows, blocks * 128), u8, device, stream),
-                         _empty((blocks, -(-rows // 16) * 16), u8, device, stream), (rows, cols), t)
+        b = Fp8Blocks.__new__(Fp8Blocks)
+        b._set(_empty((rows, blocks * 128), u8, device, stream), _empty((blocks, -(-rows // 16) * 16), u8, device, stream),
+               (rows, cols), t)
+        return b
 
 
 def _blocks(b, what, rows=None, cols=None):
+    """Checked Fp8Blocks on a GPU; their shape."""
     if not isinstance(b, Fp8Blocks):
         raise ValueError(f"{what} must be Fp8Blocks (quantize_blocks makes them), got {type(b).__name__}")
-    if not b.codes.is_cuda:
-        raise ValueError(f"{what} must be on a GPU, got {b.codes.device}")
-    want = (b.shape[0] if rows is None else rows, b.shape[1] if cols is None else cols)
-    if b.shape != want:
-        raise ValueError(f"{what} must be {want}, got {b.shape}")
-    return b
+    if b.device.type != "cuda":
+        raise ValueError(f"{what} must be on a GPU, got {b.device}")
+    m, k = b.shape
+    if (rows is not None and m != rows) or (cols is not None and k != cols):
+        raise ValueError(f"{what} must be {(m if rows is None else rows, k if cols is None else cols)}, got {(m, k)}")
+    return m, k
 
 
 def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) -> Fp8Blocks:
@@ -609,7 +618,7 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
         _blocks(out, "out", M, K)
         if transposed:
             _blocks(out.t, "out.t", K, M)
-        _same_device(dev, out=out.codes)
+        _same_device(dev, out=out)
     _call(lib().rc_quantize_blocks, dev, stream, M, K, x.data_ptr(), ldx, int(square), ctypes.byref(out.c),
           ctypes.byref(out.t.c) if transposed else None)
     return out
@@ -617,8 +626,8 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
 
 def dequantize_blocks(x, out=None, stream=None):
     """The values of Fp8Blocks in bf16 [M, K] (exact).  Returns out."""
-    M, K = _blocks(x, "x").shape
-    dev = x.codes.device
+    M, K = _blocks(x, "x")
+    dev = x.device
     if out is None:
         out = _empty((M, K), _torch().bfloat16, dev, stream)
     elif out.shape != (M, K):
@@ -638,9 +647,9 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     torch, L = _torch(), lib()
     blocks = isinstance(a, Fp8Blocks)
     lda = 0 if blocks else _rows_view(a, "a")
-    M, K = a.shape
-    dev = _blocks(a, "a").codes.device if blocks else a.device
-    N = _blocks(w, "w", cols=K).shape[0]
+    M, K = _blocks(a, "a") if blocks else a.shape
+    dev = a.device
+    N = _blocks(w, "w", cols=K)[0]
     if out is None:
         out = _empty((M, N), torch.bfloat16, dev, stream)
     for name, t in (("out", out), ("residual", residual)):
@@ -648,7 +657,7 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
             raise ValueError(f"{name} must have shape {(M, N)}, got {tuple(t.shape)}")
     ldo = _rows_view(out, "out")
     ldr = _rows_view(residual, "residual") if residual is not None else 0
-    _same_device(dev, w=w.codes, out=out, residual=residual)
+    _same_device(dev, w=w, out=out, residual=residual)
     if blocks:
         _call(L.rc_linear_fp8_blocks, dev, stream, M, N, K, ctypes.byref(a.c), ctypes.byref(w.c), _ptr(residual), ldr,
               out.data_ptr(), ldo)
@@ -677,12 +686,13 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
         raise ValueError("residual goes with dx")
     if (dx is not None and not want_dx) or (dw is not None and not want_dw):
         raise ValueError("dx or dw is given but not wanted")
-    K = (_blocks(w, "w", rows=N) if want_dx else _blocks(x, "x", rows=M)).shape[1]
+    K = (_blocks(w, "w", rows=N) if want_dx else _blocks(x, "x", rows=M))[1]
     w_t = None
     if want_dx:
         if w.t is None:
             raise ValueError("w has no transposed form: quantize_blocks(w, square=True, transposed=True)")
-        w_t = _blocks(w.t, "w.t", K, N)
+        w_t = w.t
+        _blocks(w_t, "w.t", K, N)
         if dx is None:
             dx = _empty((M, K), torch.bfloat16, dev, stream)
         for name, t in (("dx", dx), ("residual", residual)):
@@ -695,7 +705,7 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
         _expect(dw, (N, K), "torch.float32", "dw")
     lddx = _rows_view(dx, "dx") if want_dx else 0
     ldr = _rows_view(residual, "residual") if residual is not None else 0
-    _same_device(dev, dx=dx, dw=dw, residual=residual, x=x.codes if want_dw else None, w=w_t.codes if want_dx else None)
+    _same_device(dev, dx=dx, dw=dw, residual=residual, x=x if want_dw else None, w=w_t)
     need = L.rc_linear_fp8_backward_workspace_bytes(M, N, K, int(want_dx), int(want_dw))
     workspace = _workspace(workspace, need, dev, stream)
     _call(L.rc_linear_fp8_backward, dev, stream, M, N, K, dy.data_ptr(), lddy, ctypes.byref(x.c) if want_dw else None,

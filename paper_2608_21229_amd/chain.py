@@ -29,6 +29,16 @@ With ``cache="fp8"`` each layer's reference cache is stored as e4m3 codes
 with per-(batch, head) scales (``ref_kv_prefill_fp8`` /
 ``step_masked_attention_fp8``); the computation stays bf16.
 
+With ``linear="fp8"`` the projections are products of e4m3 codes with a
+power-of-two scale per block of 128 (``linear_fp8``): the weights are quantised
+once, squares with their transposed form, and every call's rows on the way.
+``full_backward`` then takes the inputs' gradients by the same products, and the
+weights' from the codes that the forward pass has read, which are the exact
+operands.  With ``checkpoints="fp8"`` it also keeps in 8 bits what it only reads
+again elementwise (the projections' inputs, the branch and the rows of the norms,
+queries and keys before their norm), at one rounding of 2^-4 relative each; the
+attention's own operands stay bf16.
+
 Every multiply-add runs in librefcache.  Work buffers come from torch's
 allocator; ``collect`` (a list) receives a copy of the hidden state after each
 layer.  ``full_backward`` also copies with torch: the weights transposed, and for
@@ -54,17 +64,23 @@ class Chain:
     chain as long as a graph that captured its calls is replayed);
     q_norms, k_norms: a [D] weight per layer; modulated: every call takes
     ``modulation`` [B, groups, layers, 3, H D] (shift, scale, gate per layer):
-    one group for prefill and step, two (live, static) for full."""
+    one group for prefill and step, two (live, static) for full.
+    linear: "bf16" or "fp8", whose weights are quantised here (``update_weights``
+    after changing them); checkpoints: what full_backward keeps, "bf16" or "fp8"."""
 
     def __init__(self, layout: rcb.Layout, w_qkv: Sequence, w_o: Sequence, H: int, D: int,
                  scale: Optional[float] = None, cache: str = "bf16", rotary: Optional[rcb.Rotary] = None,
                  positions=None, q_norms: Optional[Sequence] = None, k_norms: Optional[Sequence] = None,
-                 modulated: bool = False, norm: str = "layer", eps: float = 1e-6):
+                 modulated: bool = False, norm: str = "layer", eps: float = 1e-6, linear: str = "bf16",
+                 checkpoints: str = "bf16"):
         if len(w_qkv) != len(w_o) or not w_qkv:
             raise ValueError("need one W_qkv and one W_o per layer")
         if cache not in ("bf16", "fp8"):
             raise ValueError(f"cache must be 'bf16' or 'fp8', got {cache!r}")
-        self.cache = cache
+        for name, value in (("linear", linear), ("checkpoints", checkpoints)):
+            if value not in ("bf16", "fp8"):
+                raise ValueError(f"{name} must be 'bf16' or 'fp8', got {value!r}")
+        self.cache, self.linear, self.checkpoints = cache, linear, checkpoints
         C = H * D
         for l, (wq, wo) in enumerate(zip(w_qkv, w_o)):
             if tuple(wq.shape) != (3 * C, C) or tuple(wo.shape) != (C, C):
@@ -93,6 +109,34 @@ class Chain:
             # gathered on the stream that is current here, read on every call's
             if positions.is_cuda:
                 rcb._torch().cuda.current_stream(positions.device).synchronize()
+
+        self._w8 = None
+        if linear == "fp8":
+            self.update_weights()
+
+    def update_weights(self):
+        """Quantises the weights again (linear="fp8"), in place: calls after this one, and replays
+        of graphs that captured calls, read the new ones.  Waits for the stream that is current here,
+        on which it runs; the caller orders it after earlier calls on other streams."""
+        if self.linear != "fp8":
+            raise ValueError("update_weights needs a Chain with linear='fp8'")
+        pairs = list(zip(self.w_qkv, self.w_o))
+        old = self._w8 or [(None, None)] * len(pairs)
+        self._w8 = [tuple(rcb.quantize_blocks(w, square=True, transposed=True, out=out) for w, out in zip(ws, outs))
+                    for ws, outs in zip(pairs, old)]
+        # written on the stream that is current here, read on every call's
+        stream = rcb._torch().cuda.current_stream(self.w_o[0].device)
+        if not old[0][0]:
+            self._w8_stream = stream  # whose memory they are
+        stream.synchronize()
+
+    def _project(self, x, l: int, which: int, residual=None, out=None, stream=None):
+        """x W^T (+ residual) with W_qkv (which 0) or W_o (1); the codes of x that it has
+        read (linear="fp8") come second."""
+        if self.linear == "bf16":
+            return rcb.linear(x, (self.w_qkv, self.w_o)[which][l], residual=residual, out=out, stream=stream), None
+        x8 = rcb.quantize_blocks(x, stream=stream)
+        return rcb.linear_fp8(x8, self._w8[l][which], residual=residual, out=out, stream=stream), x8
 
     def _rows_of(self, t, which: int):
         """The rows of a class out of a tensor over all tokens."""
@@ -137,12 +181,18 @@ class Chain:
             yield lambda *ts: [t.record_stream(caller) for t in ts]
 
     def _read_positions(self, rows_kind: int, dev):
-        """Marks a call's positions as read on the stream that is current (with
+        """Marks a call's positions and 8-bit weights as read on the stream that is current (with
         stream= the call's): they belong to the constructor's, nobody but the
         chain holds them, and it may be dropped before they have been read."""
         t = self._positions.get(rows_kind)
         if t is not None and t.device == dev:  # elsewhere: the rotation refuses them
             t.record_stream(rcb._torch().cuda.current_stream(dev))
+        if self._w8 is None or self._w8_stream == rcb._torch().cuda.current_stream(dev):
+            return
+        for w8 in (w for pair in self._w8 for w in pair):  # the chain's, too
+            if w8.device == dev:
+                for t in (w8.codes, w8.exps, w8.t.codes, w8.t.exps):
+                    t.record_stream(rcb._torch().cuda.current_stream(dev))
 
     def _check_rows(self, h, rows_kind: int):
         if h.dim() != 3 or h.shape[2] != self.C:
@@ -187,12 +237,12 @@ class Chain:
             return self._modulated_layers(h, rows_kind, attend, collect, last_out, stream, mod, B, N, qkv, o, work)
         src = h.reshape(B * N, self.C)
         for l in range(self.layers):
-            rcb.linear(src, self.w_qkv[l], out=qkv, stream=stream)
+            self._project(src, l, 0, out=qkv, stream=stream)
             q, k, v = self._qkv_views(qkv, B, N)
             self._rotate(l, q, k, rows_kind, stream)
             attend(l, q, k, v, o)
             if l + 1 < self.layers or last_out or collect is not None:
-                rcb.linear(o.view(B * N, self.C), self.w_o[l], residual=src, out=work, stream=stream)
+                self._project(o.view(B * N, self.C), l, 1, residual=src, out=work, stream=stream)
                 src = work
                 if collect is not None:
                     collect.append(work.view(B, N, self.C).clone())
@@ -207,14 +257,14 @@ class Chain:
                        stream=stream)
         out = None  # the hidden state from the first layer's residual on
         for l in range(self.layers):
-            rcb.linear(y.view(B * N, self.C), self.w_qkv[l], out=qkv, stream=stream)
+            self._project(y.view(B * N, self.C), l, 0, out=qkv, stream=stream)
             q, k, v = self._qkv_views(qkv, B, N)
             self._rotate(l, q, k, rows_kind, stream)
             attend(l, q, k, v, o)
             last = l + 1 == self.layers
             if last and not last_out and collect is None:
                 break
-            rcb.linear(o.view(B * N, self.C), self.w_o[l], out=work, stream=stream)
+            self._project(o.view(B * N, self.C), l, 1, out=work, stream=stream)
             nxt = {} if last else dict(scale=mod[:, :, l + 1, 1], shift=mod[:, :, l + 1, 0], y=y)
             h, _ = rcb.gated_norm(h, branch, gate=mod[:, :, l, 2], norm=self.norm, eps=self.eps, spans=spans, h_out=out,
                                   want_y=not last, stream=stream, **nxt)
@@ -292,8 +342,9 @@ class Chain:
         """Gradient of ``full``: dh [B, N, H D] is the gradient of its result.
         Runs the layers forward, keeping their activations, and back.  Returns
         ChainGrads(h, w_qkv, w_o, q_norms, k_norms, modulation): the hidden
-        state's and the weights' in bf16, the norms' and the modulation's in
-        fp32 (None where the chain has none)."""
+        state's and the weights' in bf16 (those from 8-bit operands or checkpoints
+        in fp32), the norms' and the modulation's in fp32 (None where the chain
+        has none)."""
         with self._scope(stream, h.device) as returned:
             grads = self._full_backward(h, dh, modulation, stream)
             for g in grads:
@@ -311,30 +362,40 @@ class Chain:
         self._read_positions(rcb.ROWS_ALL, h.device)
         spans = self._spans(rcb.ROWS_ALL)
         norm = dict(norm=self.norm, eps=self.eps, spans=spans, stream=stream)
+        fp8 = self.checkpoints == "fp8"
         kept, h = [], h.contiguous()
         first = h
         y = h if mod is None else rcb.gated_norm(h, scale=mod[:, :, 0, 1], shift=mod[:, :, 0, 0], **norm)[1]
         for l in range(self.layers):
-            qkv = rcb.linear(y.view(M, C), self.w_qkv[l], stream=stream)
+            qkv, y8 = self._project(y.view(M, C), l, 0, stream=stream)
             q, k, v = self._qkv_views(qkv, B, N)
             turned = qkv
-            if self.q_norms is not None:  # the norm's gradient reads its inputs
+            if self.q_norms is not None and fp8:  # the norm's gradient reads its inputs
+                before = rcb.quantize_blocks(qkv[:, :2 * C], stream=stream)
+            elif self.q_norms is not None:
                 turned = qkv.clone()
             elif self.rotary is not None:
                 qkv = None
             qt, kt, vt = self._qkv_views(turned, B, N)
             self._rotate(l, q, k, rcb.ROWS_ALL, stream, qt, kt)
+            if self.q_norms is not None and fp8:
+                qkv = before
             o, lse = rcb.full_attention(self.layout, qt, kt, vt, scale=self.scale, want_lse=True, stream=stream)
             last = l + 1 == self.layers
             if mod is None:
-                branch, at = None, h
-                h = y_next = rcb.linear(o.view(M, C), self.w_o[l], residual=h.view(M, C), stream=stream).view(B, N, C)
+                branch, at = None, None
+                h = self._project(o.view(M, C), l, 1, residual=h.view(M, C), stream=stream)[0].view(B, N, C)
+                y_next = h
             else:
-                branch = rcb.linear(o.view(M, C), self.w_o[l], stream=stream).view(B, N, C)
+                branch = self._project(o.view(M, C), l, 1, stream=stream)[0].view(B, N, C)
                 nxt = {} if last else dict(scale=mod[:, :, l + 1, 1], shift=mod[:, :, l + 1, 0])
                 at, y_next = rcb.gated_norm(h, branch, gate=mod[:, :, l, 2], want_y=not last, **nxt, **norm)
                 h = at
-            kept.append((y, qkv, turned, o, lse, branch, at))
+                if fp8:
+                    branch, at = (rcb.quantize_blocks(t.view(M, C), stream=stream) for t in (branch, at))
+            if fp8 and y8 is None:
+                y8 = rcb.quantize_blocks(y.view(M, C), stream=stream)
+            kept.append((y if y8 is None else y8, qkv, turned, o, lse, branch, at))
             y = y_next
 
         d_qkv, d_o = [None] * self.layers, [None] * self.layers
@@ -350,30 +411,47 @@ class Chain:
                 da = dh
             else:
                 nxt = {} if last else dict(scale=mod[:, :, l + 1, 1], shift=mod[:, :, l + 1, 0])
+                if fp8:
+                    at, branch = (rcb.dequantize_blocks(t, stream=stream).view(B, N, C) for t in (at, branch))
                 g = rcb.gated_norm_backward(dy, at, branch, dh=dh, gate=mod[:, :, l, 2], **nxt, **norm)
                 dh, da, dmod[:, :, l, 2] = g.h, g.x, g.gate
                 if not last:
                     dmod[:, :, l + 1, 0], dmod[:, :, l + 1, 1] = g.shift, g.scale
-            d_o[l] = _weight_grad(da.view(M, C), o.view(M, C), stream)
-            do = rcb.linear(da.view(M, C), self.w_o[l].t().contiguous(), stream=stream).view(B, N, self.H, self.D)
+            if self.linear == "fp8":
+                # the codes that the forward product read, made again: o is kept for the attention's gradient
+                o8 = rcb.quantize_blocks(o.view(M, C), stream=stream)
+                do, d_o[l] = rcb.linear_fp8_backward(da.view(M, C), o8, self._w8[l][1], stream=stream)
+            else:
+                d_o[l] = _weight_grad(da.view(M, C), o.view(M, C), stream)
+                do = rcb.linear(da.view(M, C), self.w_o[l].t().contiguous(), stream=stream)
+            do = do.view(B, N, self.H, self.D)
             q, k, v = self._qkv_views(turned, B, N)
             dqkv = torch.empty_like(turned)
             dq, dk, dv = self._qkv_views(dqkv, B, N)
             rcb.full_attention_backward(self.layout, q, k, v, o, lse, do, dq, dk, dv, scale=self.scale, stream=stream)
             if self.rotary is not None:
                 q_norm, k_norm = self._norms(l)
-                q0, k0 = (None, None) if q_norm is None else self._qkv_views(qkv, B, N)[:2]
+                q0 = k0 = None
+                if q_norm is not None and fp8:
+                    q0, k0 = rcb.dequantize_blocks(qkv, stream=stream).view(B, N, 2, self.H, self.D).unbind(2)
+                elif q_norm is not None:
+                    q0, k0 = self._qkv_views(qkv, B, N)[:2]
                 _, _, gq, gk = rcb.qk_rotary_backward(self.rotary, dq, dk, self._positions[rcb.ROWS_ALL], q=q0, k=k0,
                                                       q_norm=q_norm, k_norm=k_norm, eps=self.eps, dq_out=dq, dk_out=dk,
                                                       stream=stream)
                 if q_norm is not None:
                     dq_norms[l], dk_norms[l] = gq, gk
-            d_qkv[l] = _weight_grad(dqkv, y.reshape(M, C), stream)
-            w_t = self.w_qkv[l].t().contiguous()
-            if mod is None:
-                dh = rcb.linear(dqkv, w_t, residual=dh.view(M, C), stream=stream).view(B, N, C)
+            through = dh.view(M, C) if mod is None else None
+            if self.linear == "fp8":
+                dx, d_qkv[l] = rcb.linear_fp8_backward(dqkv, y, self._w8[l][0], residual=through, stream=stream)
             else:
-                dy = rcb.linear(dqkv, w_t, stream=stream).view(B, N, C)
+                d_qkv[l] = (rcb.linear_fp8_backward(dqkv, y, None, want_dx=False, stream=stream)[1] if fp8
+                            else _weight_grad(dqkv, y.reshape(M, C), stream))
+                dx = rcb.linear(dqkv, self.w_qkv[l].t().contiguous(), residual=through, stream=stream)
+            if mod is None:
+                dh = dx.view(B, N, C)
+            else:
+                dy = dx.view(B, N, C)
         if mod is not None:
             g = rcb.gated_norm_backward(dy, first, dh=dh, scale=mod[:, :, 0, 1], shift=mod[:, :, 0, 0], **norm)
             dh, dmod[:, :, 0, 0], dmod[:, :, 0, 1] = g.h, g.shift, g.scale

@@ -1480,7 +1480,7 @@ rc_status run_linear8(int64_t M, int32_t N, int32_t K, Linear8Params& q, const v
   q.M = M;
   q.N = N;
   q.K = K;
-  if (q.x && M <= kFewRows8) return hip_status(launch_linear8_few(q, stream), "FP8 linear launch");
+  if (q.x && few_rows8(M, N, K)) return hip_status(launch_linear8_few(q, stream), "FP8 linear launch");
   if (q.x) {
     q.a = blocks_in(workspace, M, K);
     const Quant8Params z{q.x, q.ldx, M, K, q.a, Blocks8{nullptr, 0, nullptr, 0}};
@@ -1500,12 +1500,7 @@ rc_status check_out8(int64_t N, const void* r, int64_t ldr, const void* out, int
   return RC_OK;
 }
 
-size_t linear8_workspace(int64_t M, int64_t K) { return M <= kFewRows8 ? 0 : blocks8_bytes(M, K); }
-
-size_t wgrad8_partial_bytes(int64_t M, int32_t N, int32_t K) {
-  const int32_t splits = plan_wgrad8(M, N, K).splits;
-  return splits > 1 ? size_t(splits) * N * K * sizeof(float) : 0;
-}
+size_t linear8_workspace(int64_t M, int32_t N, int32_t K) { return few_rows8(M, N, K) ? 0 : blocks8_bytes(M, K); }
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -1568,7 +1563,7 @@ rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8
 
 size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K) {
   using namespace rc;
-  return check_size8("FP8 linear", M, N, K) == RC_OK ? linear8_workspace(M, K) : 0;
+  return check_size8("FP8 linear", M, N, K) == RC_OK ? linear8_workspace(M, N, K) : 0;
 }
 
 rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const rc_blocks8* w,
@@ -1582,7 +1577,7 @@ rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t 
   RC_TRY(check_blocks8(w, N, K, "w"));
   RC_TRY(check_out8(N, r, ldr, out, ldo));
   RC_TRY(check_grid8(M, N, K, "FP8 linear"));
-  RC_TRY(check_workspace8("FP8 linear", workspace, ws_bytes, linear8_workspace(M, K)));
+  RC_TRY(check_workspace8("FP8 linear", workspace, ws_bytes, linear8_workspace(M, N, K)));
   RC_TRY(check_launcher(launch_linear8, "FP8 linear"));
   Linear8Params q{};
   q.x = static_cast<const uint16_t*>(a);
@@ -1594,7 +1589,7 @@ rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t 
 size_t rc_linear_fp8_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t want_dx, int32_t want_dw) {
   using namespace rc;
   if (check_size8("FP8 linear's gradient", M, N, K) != RC_OK) return 0;
-  return (want_dx ? round16(linear8_workspace(M, N)) : 0) + (want_dw ? wgrad8_partial_bytes(M, N, K) : 0);
+  return (want_dx ? round16(linear8_workspace(M, K, N)) : 0) + (want_dw ? plan_wgrad8(M, N, K).partial_bytes() : 0);
 }
 
 rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy, int64_t lddy, const rc_blocks8* x,
@@ -1624,8 +1619,8 @@ rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy
     RC_TRY(check_ptr(dw, "dw"));
     RC_TRY(check_ld8(lddw, K, "dw"));
     if (M > 0) RC_TRY(check_blocks8(x, M, K, "x"));
-    RC_TRY(check_blocks((int64_t(N) + 127) / 128 * ((K + 127) / 128) * plan_wgrad8(M, N, K).splits, "FP8 weights' gradient"));
-    RC_TRY(check_blocks((int64_t(N) * (K / 4) + 255) / 256, "FP8 weights' gradient"));
+    const WGrad8Plan plan = plan_wgrad8(M, N, K);
+    RC_TRY(check_blocks(plan.blocks(), "FP8 weights' gradient"));
   }
   RC_TRY(check_workspace8("FP8 linear's gradient", workspace, ws_bytes,
                           rc_linear_fp8_backward_workspace_bytes(M, N, K, dx != nullptr, dw != nullptr)));
@@ -1646,10 +1641,11 @@ rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy
     if (M > 0) q.x = blocks_of(x);
     q.dw = dw;
     q.lddw = lddw;
-    q.partial = reinterpret_cast<float*>(ws + (dx ? round16(linear8_workspace(M, N)) : 0));
+    q.partial = reinterpret_cast<float*>(ws + (dx ? round16(linear8_workspace(M, K, N)) : 0));
     q.M = M;
     q.N = N;
     q.K = K;
+    q.whole = plan.whole;
     q.splits = plan.splits;
     RC_TRY(hip_status(launch_wgrad8(q, plan.tile, stream), "FP8 weights' gradient launch"));
   }

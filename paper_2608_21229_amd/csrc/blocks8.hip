@@ -54,38 +54,48 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const Quant8Params q
   }
 }
 
-// Squares of 128 x 128, one per work-group; the transposed codes go through
-// LDS.  Rows and columns up to the next multiple of 128 exist as zeros.
+// 4 x 4 bytes, rows to columns.
+__device__ __forceinline__ void transpose4(uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t (&c)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(r1, r0, 0x05010400u), b = __builtin_amdgcn_perm(r1, r0, 0x07030602u);
+  const uint32_t d = __builtin_amdgcn_perm(r3, r2, 0x05010400u), e = __builtin_amdgcn_perm(r3, r2, 0x07030602u);
+  c[0] = __builtin_amdgcn_perm(d, a, 0x05040100u);
+  c[1] = __builtin_amdgcn_perm(d, a, 0x07060302u);
+  c[2] = __builtin_amdgcn_perm(e, b, 0x05040100u);
+  c[3] = __builtin_amdgcn_perm(e, b, 0x07060302u);
+}
+
+// Squares of 128 x 128, one per work-group, 8 x 8 values per thread, whose
+// codes are transposed in registers; LDS only gathers them into whole rows (8-byte
+// part p of row k at part p ^ (k / 8)).  Columns up to the next multiple of 128 exist
+// as zeros.  Memory-bound: 2 bytes read and 1 or 2 written per value.
 __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Params q) {
-  constexpr int kPitch = kBlock8 + 8;
-  __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kPitch];
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kBlock8];
   __shared__ float red[4];
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, c8 = t & 15, r8 = t >> 4;
   const int kblocks = (q.K + kBlock8 - 1) / kBlock8;
   const int64_t nb = int64_t(blockIdx.x) / kblocks;
   const int kb = int(blockIdx.x % kblocks);
   const int64_t m0 = nb * kBlock8, k0 = int64_t(kb) * kBlock8;
-  const int64_t col = k0 + (t & 15) * 8;
+  const int64_t col = k0 + c8 * 8, row = m0 + r8 * 8;
   u32x4 v[8];
   float a = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int64_t m = m0 + i * 16 + (t >> 4);
     v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (m < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + col);
-    a = fmaxf(a, finite_amax8(v[i]));
+    if (row + i < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + (row + i) * q.ldx + col);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_amax8(v[i]));
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
   if ((t & 63) == 0) red[t >> 6] = a;
   __syncthreads();
   const uint32_t byte = exponent_byte(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  u32x2 c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int row = i * 16 + (t >> 4);
-    const u32x2 c = codes8(v[i], byte);
-    if (m0 + row < q.M) *reinterpret_cast<u32x2*>(q.out.codes + (m0 + row) * q.out.ld + col) = c;
-    if (q.out_t.codes) *reinterpret_cast<u32x2*>(tile + row * kPitch + (t & 15) * 8) = c;
+    c[i] = codes8(v[i], byte);
+    if (row + i < q.M) *reinterpret_cast<u32x2*>(q.out.codes + (row + i) * q.out.ld + col) = c[i];
   }
   const uint32_t four = byte * 0x01010101u;
   if (t < 32) {
@@ -95,14 +105,22 @@ __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Param
     if (k0 + r < q.out_t.le) *reinterpret_cast<uint32_t*>(q.out_t.exps + nb * q.out_t.le + k0 + r) = four;
   }
   if (!q.out_t.codes) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t lo[4], hi[4];
+    transpose4(c[0][h], c[1][h], c[2][h], c[3][h], lo);
+    transpose4(c[4][h], c[5][h], c[6][h], c[7][h], hi);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<u32x2*>(tile + (c8 * 8 + 4 * h + e) * kBlock8 + (r8 ^ c8) * 8) = u32x2{lo[e], hi[e]};
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int k = i * 16 + (t >> 4), n = (t & 15) * 8;
-    u32x2 c{0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e / 4] |= uint32_t(tile[(n + e) * kPitch + k]) << (8 * (e & 3));
-    if (k0 + k < q.K) *reinterpret_cast<u32x2*>(q.out_t.codes + (k0 + k) * q.out_t.ld + m0 + n) = c;
+    const int k = i * 16 + (t >> 4), n8 = t & 15;
+    if (k0 + k < q.K)
+      *reinterpret_cast<u32x2*>(q.out_t.codes + (k0 + k) * q.out_t.ld + m0 + n8 * 8) =
+          *reinterpret_cast<const u32x2*>(tile + k * kBlock8 + (n8 ^ (k >> 3)) * 8);
   }
 }
 

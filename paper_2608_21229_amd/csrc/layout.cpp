@@ -504,7 +504,7 @@ LinearPlan plan_linear(const LinearParams& q) {
 int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
   struct {
     int64_t fixed, slice;
-  } constexpr kCost[] = {{5500, 1475}, {3700, 806}, {3200, 473}, {2500, 380}, {1800, 223}};
+  } constexpr kCost[] = {{6000, 1400}, {4000, 780}, {3500, 500}, {3000, 370}, {2500, 280}};
   int32_t best = 0;
   int64_t best_cost = INT64_MAX;
   for (int32_t i = 0; i < 5; ++i) {
@@ -519,18 +519,33 @@ int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
   return best;
 }
 
-// The tile of a weights' gradient, and the shares of the rows where the tiles
-// alone leave CUs idle.
+// How a weights' gradient runs: the tile size, and the shares of the rows for
+// the tiles of a partial last round, by their cost in ns.
 WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K) {
-  WGrad8Plan p{0, 1};
-  const auto tiles = [&](int32_t i) {
+  struct {
+    int64_t fixed, slice;
+  } constexpr kCost[] = {{5500, 1300}, {5000, 930}, {4000, 690}};
+  const int64_t slices = (M + 63) / 64;
+  WGrad8Plan best{0, 1, 0, 0};
+  int64_t best_cost = INT64_MAX;
+  for (int32_t i = 0; i < 3; ++i) {
     const Tile8& t = kWGrad8Tiles[i];
-    return int64_t((N + t.bm - 1) / t.bm) * ((K + t.bn - 1) / t.bn);
-  };
-  if (tiles(0) < kCUs / 2) p.tile = 1;
-  const int64_t slices = (M + 63) / 64, n = tiles(p.tile);
-  if (n < kCUs) p.splits = int32_t(std::max<int64_t>(1, std::min<int64_t>(kCUs / n, slices / 4)));
-  return p;
+    const auto& c = kCost[i];
+    const int64_t tiles = int64_t((N + t.bm - 1) / t.bm) * ((K + t.bn - 1) / t.bn);
+    const int64_t whole = tiles / kCUs * kCUs, rest = tiles - whole;
+    const int64_t most = rest > 0 ? std::max<int64_t>(1, std::min(kCUs / rest, slices)) : 1;
+    for (int64_t j = 1; j <= most; ++j) {
+      const int64_t bytes = int64_t(t.bm) * t.bn * 4, rate = 5000;  // of a tile; bytes per ns
+      int64_t cost = whole / kCUs * (c.fixed + slices * c.slice + kCUs * bytes / rate);
+      if (rest > 0) cost += c.fixed + (slices + j - 1) / j * c.slice + j * rest * bytes / rate;
+      if (j > 1) cost += 4000 + j * rest * bytes / rate;  // the join
+      if (cost < best_cost) {
+        best_cost = cost;
+        best = WGrad8Plan{i, int32_t(j), whole, tiles};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace rc

@@ -198,82 +198,119 @@ __global__ __launch_bounds__(WM * WN * 64) void linear8_kernel(const Linear8Para
   __shared__ __attribute__((aligned(1024))) char ring[ST * (BM + BN) * kBK];
   __shared__ __attribute__((aligned(1024))) char scales[kScaleRing<BM, BN>];
   int64_t row, col;
-  grouped_tile(xcd_block(blockIdx.x, gridDim.x), (q.M + BM - 1) / BM, (q.N + BN - 1) / BN, 4, row, col);
+  grouped_tile<int64_t>(xcd_block(blockIdx.x, gridDim.x), (q.M + BM - 1) / BM, (q.N + BN - 1) / BN, 4, row, col);
   product8_tile<MB, NB, WM, WN, ST>(q, ring, scales, row * BM, int(col * BN));
 }
 
-// Few rows (M <= 16): reading W is the work, and the rows are quantised on the
-// way.  A work-group takes 32 columns, its eight waves a share of the slices
-// each; a wave reads a slice of W and of the rows straight into the operands of
-// v_mfma_scale_f32_16x16x128 (lane: row lane % 16, 32 of the slice's 128
-// values), the four lanes of a row agree on the block's maximum, and the waves'
-// sums are added in order through LDS.
+// Few rows, or a small product: reading W is the work, or the launch, and the rows
+// are quantised on the way.  A work-group takes 16 MT rows and 32 columns, its
+// eight waves a share of the slices each; a wave reads a slice of W and of the rows
+// straight into the operands of v_mfma_scale_f32_16x16x128 (lane: row lane % 16, 32
+// of the slice's 128 values), the next slice's loads ahead; the four lanes of a row
+// agree on the block's maximum, and the waves' sums are added in order through LDS.
 constexpr int kFewWaves = 8, kFewTiles = 2;
 
+template <int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void linear8_few_kernel(const Linear8Params q) {
-  __shared__ f32x4 sums[kFewWaves][kFewTiles][64];
+  __shared__ f32x4 sums[kFewWaves][MT][kFewTiles][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 15, quarter = lane >> 4;
   const int n0 = int(blockIdx.x) * 16 * kFewTiles;
+  const int64_t m0 = int64_t(blockIdx.y) * 16 * MT;
   const int steps = int(blocks8(q.K));
-  f32x4 acc[kFewTiles];
-#pragma unroll
-  for (int t = 0; t < kFewTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int s = wave; s < steps; s += kFewWaves) {
-    const int64_t k = int64_t(s) * kBK + quarter * 32;
-    u32x4 w[kFewTiles][2], x[4];
+  struct Slice {
+    u32x4 w[kFewTiles][2], x[MT][4];
     int ew[kFewTiles];
+  };
+  const uint8_t *pw[kFewTiles], *pe[kFewTiles];
+#pragma unroll
+  for (int t = 0; t < kFewTiles; ++t) {
+    const int64_t n = min(n0 + t * 16 + row, q.N - 1);  // columns past the last are not stored
+    pw[t] = q.w.codes + n * q.w.ld + quarter * 32;
+    pe[t] = q.w.exps + n;
+  }
+  const auto load = [&](Slice& z, int s) {
+    const int64_t k = int64_t(s) * kBK;
 #pragma unroll
     for (int t = 0; t < kFewTiles; ++t) {
-      const int n = min(n0 + t * 16 + row, q.N - 1);  // columns past the last are not stored
-      w[t][0] = *reinterpret_cast<const u32x4*>(q.w.codes + n * q.w.ld + k);
-      w[t][1] = *reinterpret_cast<const u32x4*>(q.w.codes + n * q.w.ld + k + 16);
-      ew[t] = q.w.exps[s * q.w.le + n];
+      z.w[t][0] = *reinterpret_cast<const u32x4*>(pw[t] + k);
+      z.w[t][1] = *reinterpret_cast<const u32x4*>(pw[t] + k + 16);
+      z.ew[t] = pe[t][s * q.w.le];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = u32x4{0u, 0u, 0u, 0u};
-      if (row < q.M && k + 8 * i < q.K) x[i] = *reinterpret_cast<const u32x4*>(q.x + row * q.ldx + k + 8 * i);
-    }
-    float a = 0.f;
+    for (int u = 0; u < MT; ++u) {
+      const int64_t m = m0 + u * 16 + row, c = k + quarter * 32;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a = fmaxf(a, finite_amax8(x[i]));
-    a = fmaxf(a, __shfl_xor(a, 16));
-    a = fmaxf(a, __shfl_xor(a, 32));
-    const uint32_t byte = exponent_byte(a);
-    u32x8 fx;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x2 c = codes8(x[i], byte);
-      fx[2 * i] = c[0];
-      fx[2 * i + 1] = c[1];
+      for (int i = 0; i < 4; ++i) {
+        z.x[u][i] = u32x4{0u, 0u, 0u, 0u};
+        if (m < q.M && c + 8 * i < q.K) z.x[u][i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + c + 8 * i);
+      }
     }
+  };
+  f32x4 acc[MT][kFewTiles];
 #pragma unroll
-    for (int t = 0; t < kFewTiles; ++t) {
-      const u32x8 fw = __builtin_shufflevector(w[t][0], w[t][1], 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, fw), __builtin_bit_cast(i32x8, fx),
-                                                                acc[t], 0, 0, 0, ew[t], 0, int(byte));
+  for (int u = 0; u < MT; ++u)
+#pragma unroll
+    for (int t = 0; t < kFewTiles; ++t) acc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto add = [&](const Slice& z) {
+#pragma unroll
+    for (int u = 0; u < MT; ++u) {
+      float a = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a = fmaxf(a, finite_amax8(z.x[u][i]));
+      a = fmaxf(a, __shfl_xor(a, 16));
+      a = fmaxf(a, __shfl_xor(a, 32));
+      const uint32_t byte = exponent_byte(a);
+      u32x8 fx;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x2 c = codes8(z.x[u][i], byte);
+        fx[2 * i] = c[0];
+        fx[2 * i + 1] = c[1];
+      }
+#pragma unroll
+      for (int t = 0; t < kFewTiles; ++t) {
+        const u32x8 fw = __builtin_shufflevector(z.w[t][0], z.w[t][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[u][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            __builtin_bit_cast(i32x8, fw), __builtin_bit_cast(i32x8, fx), acc[u][t], 0, 0, 0, z.ew[t], 0, int(byte));
+      }
     }
+  };
+  Slice z0, z1;
+  int s = wave;
+  if (s < steps) load(z0, s);
+  while (s < steps) {
+    if (s + kFewWaves < steps) load(z1, s + kFewWaves);
+    add(z0);
+    s += kFewWaves;
+    if (s >= steps) break;
+    if (s + kFewWaves < steps) load(z0, s + kFewWaves);
+    add(z1);
+    s += kFewWaves;
   }
 #pragma unroll
-  for (int t = 0; t < kFewTiles; ++t) sums[wave][t][lane] = acc[t];
+  for (int u = 0; u < MT; ++u)
+#pragma unroll
+    for (int t = 0; t < kFewTiles; ++t) sums[wave][u][t][lane] = acc[u][t];
   __syncthreads();
-  if (wave >= kFewTiles) return;
-  f32x4 v = sums[0][wave][lane];
+  for (int i = wave; i < MT * kFewTiles; i += kFewWaves) {
+    const int u = i / kFewTiles, t = i % kFewTiles;
+    f32x4 v = sums[0][u][t][lane];
 #pragma unroll
-  for (int i = 1; i < kFewWaves; ++i) v += sums[i][wave][lane];
-  const int64_t m = row;
-  const int n = n0 + wave * 16 + quarter * 4;  // the accumulator of 16 x 16: column lane % 16, rows 4 (lane / 16) ..
-  if (m >= q.M || n >= q.N) return;
-  if (q.r) {
-    const bf16x4 rb = *reinterpret_cast<const bf16x4*>(q.r + m * q.ldr + n);
+    for (int w = 1; w < kFewWaves; ++w) v += sums[w][u][t][lane];
+    const int64_t m = m0 + u * 16 + row;
+    const int n = n0 + t * 16 + quarter * 4;  // the accumulator of 16 x 16: column lane % 16, rows 4 (lane / 16) ..
+    if (m >= q.M || n >= q.N) continue;
+    if (q.r) {
+      const bf16x4 rb = *reinterpret_cast<const bf16x4*>(q.r + m * q.ldr + n);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += float(rb[e]);
+      for (int e = 0; e < 4; ++e) v[e] += float(rb[e]);
+    }
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
+    *reinterpret_cast<bf16x4*>(q.out + m * q.ldo + n) = o;
   }
-  bf16x4 o;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
-  *reinterpret_cast<bf16x4*>(q.out + m * q.ldo + n) = o;
 }
 
 template <int MB, int NB, int WM, int WN, int ST>
@@ -299,8 +336,11 @@ int launch_linear8(const Linear8Params& q, int32_t tile, void* stream) {
 
 int launch_linear8_few(const Linear8Params& q, void* stream) {
   constexpr int kCols = 16 * kFewTiles;
-  hipLaunchKernelGGL(linear8_few_kernel, dim3((q.N + kCols - 1) / kCols), dim3(kFewWaves * 64), 0,
-                     static_cast<hipStream_t>(stream), q);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int mt = q.M <= 16 ? 1 : 2;
+  const dim3 grid((q.N + kCols - 1) / kCols, (q.M + 16 * mt - 1) / (16 * mt)), block(kFewWaves * 64);
+  if (mt == 1) hipLaunchKernelGGL(linear8_few_kernel<1>, grid, block, 0, s, q);
+  else hipLaunchKernelGGL(linear8_few_kernel<2>, grid, block, 0, s, q);
   return int(hipGetLastError());
 }
 

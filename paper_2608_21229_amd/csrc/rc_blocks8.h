@@ -66,14 +66,22 @@ struct WGrad8Params {
   Blocks8 x;           // [M, K]
   float* dw;           // [N, K]
   int64_t lddw;
-  float* partial;      // [splits, N, K]; splits > 1
+  float* partial;      // [splits, other tiles][tile]; splits > 1
   int64_t M;
-  int32_t N, K, splits;
+  int32_t N, K;
+  int64_t whole;       // tiles that one work-group computes
+  int32_t splits;      // work-groups that share the rows of each other tile
 };
 int launch_wgrad8(const WGrad8Params& q, int32_t tile, void* stream) RC_WEAK;
 
-// Rows up to which a product quantises its bf16 rows itself.
-constexpr int64_t kFewRows8 = 16;
+// Products that quantise their bf16 rows themselves, in one launch: up to 16 rows
+// (2 x 7680 x 2560 8.1 us; the quantisation's launch and the product's 4 + 9), or
+// little to read for each group of 32 rows (80 x 384 x 128 in one launch of 4 us
+// instead of two; 32 x 7680 x 2560 14.9 us, as much as both).
+constexpr int64_t kFewRows8 = 16, kFewRead8 = int64_t(4) << 20;
+constexpr bool few_rows8(int64_t M, int32_t N, int32_t K) {
+  return M <= kFewRows8 || (M + 31) / 32 * N * pad8(K) <= kFewRead8;
+}
 
 struct Tile8 {
   int32_t bm, bn;
@@ -81,9 +89,14 @@ struct Tile8 {
 constexpr Tile8 kLinear8Tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 128}, {64, 64}};
 int32_t plan_linear8(int64_t M, int32_t N, int32_t K);
 
-constexpr Tile8 kWGrad8Tiles[] = {{256, 256}, {128, 128}};  // n x k
+constexpr Tile8 kWGrad8Tiles[] = {{256, 256}, {256, 128}, {128, 128}};  // n x k
 struct WGrad8Plan {
   int32_t tile, splits;
+  int64_t whole, tiles;
+  int64_t blocks() const { return whole + (tiles - whole) * splits; }
+  size_t partial_bytes() const {
+    return splits > 1 ? size_t(blocks() - whole) * kWGrad8Tiles[tile].bm * kWGrad8Tiles[tile].bn * sizeof(float) : 0;
+  }
 };
 WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K);
 

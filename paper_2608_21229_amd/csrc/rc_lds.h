@@ -40,12 +40,12 @@ __device__ __forceinline__ int64_t xcd_block(int64_t bid, int64_t nblk) {
 }
 
 // Logical tile w of rows x cols: groups of `group` row tiles, rows fastest inside a group.
-__device__ __forceinline__ void grouped_tile(int64_t w, int64_t rows, int64_t cols, int64_t group, int64_t& row,
-                                             int64_t& col) {
-  const int64_t per_group = group * cols;
-  const int64_t first = w / per_group * group;
-  const int64_t n = min(group, rows - first);
-  const int64_t in = w % per_group;
+template <typename Int>
+__device__ __forceinline__ void grouped_tile(Int w, Int rows, Int cols, int group, Int& row, Int& col) {
+  const Int per_group = group * cols;
+  const Int first = w / per_group * group;
+  const Int n = min(Int(group), rows - first);
+  const Int in = w % per_group;
   row = first + in % n;
   col = in / n;
 }

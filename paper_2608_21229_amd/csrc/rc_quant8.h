@@ -64,9 +64,7 @@ __device__ __forceinline__ u32x2 codes8(u32x4 g, uint32_t byte) {
 // The scale as the conversions take it: they read its exponent field.
 __device__ __forceinline__ float scale8(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// 8 codes times 2^e in bf16.
-__device__ __forceinline__ u32x4 values8(u32x2 c, uint32_t byte) {
-  const float s = scale8(byte);
+__device__ __forceinline__ u32x4 scaled_values8(u32x2 c, float s) {
   u32x4 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -74,6 +72,15 @@ __device__ __forceinline__ u32x4 values8(u32x2 c, uint32_t byte) {
     out[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, true));
   }
   return out;
+}
+
+// 8 codes times 2^e in bf16.
+__device__ __forceinline__ u32x4 values8(u32x2 c, uint32_t byte) { return scaled_values8(c, scale8(byte)); }
+
+// The same for the low byte of any bits: zeros stay zeros whatever lies in place
+// of their exponent, 255 (a scale of no number, which no block has) included.
+__device__ __forceinline__ u32x4 values8_any(u32x2 c, uint32_t bits) {
+  return scaled_values8(c, __uint_as_float(min(bits << 23 & 0x7f800000u, 0x7f000000u)));
 }
 
 }  // namespace rc
