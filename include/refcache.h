@@ -506,8 +506,8 @@ rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8
                                const void* r, int64_t ldr, void* out, int64_t ldo, void* stream);
 
 /* The same of the quantised rows of a [M, K] bf16 (blocks of a row), without handing them out.  The
- * workspace (rc_linear_fp8_workspace_bytes, 16-byte aligned) holds them; up to 16 rows need none and are
- * summed in another order than by rc_linear_fp8_blocks. */
+ * workspace (rc_linear_fp8_workspace_bytes, 16-byte aligned) holds them; calls of few rows (up to 32, or more
+ * where M N K is small) need none (0) and sum in another order than rc_linear_fp8_blocks. */
 rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const rc_blocks8* w,
                         const void* r, int64_t ldr, void* out, int64_t ldo, void* workspace, size_t ws_bytes,
                         void* stream);

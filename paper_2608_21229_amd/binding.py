@@ -643,7 +643,8 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     or bf16 (any row stride; quantised per 128 values of a row on the way, into the
     workspace); bf16 out, fp32 accumulation.  residual, out: [M, N] (any row
     stride; out may be residual).  A row's result does not depend on M for
-    Fp8Blocks; a bf16 call of up to 16 rows sums in another order.  Returns out."""
+    Fp8Blocks; a small bf16 call (up to 32 rows, or little work) sums in another order.
+    Returns out."""
     torch, L = _torch(), lib()
     blocks = isinstance(a, Fp8Blocks)
     lda = 0 if blocks else _rows_view(a, "a")

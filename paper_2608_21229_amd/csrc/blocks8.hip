@@ -10,7 +10,7 @@
 #include <stdint.h>
 
 #include "rc_blocks8.h"
-#include "rc_device.h"
+#include "rc_lds.h"
 #include "rc_quant8.h"
 
 namespace rc {
@@ -31,17 +31,19 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const Quant8Params q
   const int kb0 = int(blockIdx.x % groups) * 4;
   const int kb = kb0 + (lane >> 4);
   const int64_t col = int64_t(kb0) * kBlock8 + lane * 8;
+  const __amdgpu_buffer_rsrc_t x =
+      bytes_rsrc(q.x + m0 * q.ldx, ((min(int64_t(kRows), q.M - m0) - 1) * q.ldx + q.K) * 2);
   u32x4 v[kRows / 4];
 #pragma unroll
   for (int i = 0; i < kRows / 4; ++i) {
-    const int64_t m = m0 + i * 4 + wave;
-    v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (m < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + col);
+    v[i] = load16(x, uint32_t(i * 4 + wave) * uint32_t(q.ldx) * 2u + uint32_t(col) * 2u, col < q.K);
   }
+  uint32_t top[kRows / 4];
+  finite_abs_max(v, top);
 #pragma unroll
   for (int i = 0; i < kRows / 4; ++i) {
     const int row = i * 4 + wave;
-    const uint32_t byte = exponent_byte(group_max16(finite_amax8(v[i])));
+    const uint32_t byte = exponent_byte(group_max16(top[i]));
     if (m0 + row < q.M && kb < kblocks) *reinterpret_cast<u32x2*>(q.out.codes + (m0 + row) * q.out.ld + col) = codes8(v[i], byte);
     if ((lane & 15) == 0) exps[lane >> 4][row] = uint8_t(byte);
   }
@@ -70,27 +72,26 @@ __device__ __forceinline__ void transpose4(uint32_t r0, uint32_t r1, uint32_t r2
 // as zeros.  Memory-bound: 2 bytes read and 1 or 2 written per value.
 __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Params q) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kBlock8];
-  __shared__ float red[4];
+  __shared__ uint32_t red[4];
   const int t = threadIdx.x, c8 = t & 15, r8 = t >> 4;
   const int kblocks = (q.K + kBlock8 - 1) / kBlock8;
   const int64_t nb = int64_t(blockIdx.x) / kblocks;
   const int kb = int(blockIdx.x % kblocks);
   const int64_t m0 = nb * kBlock8, k0 = int64_t(kb) * kBlock8;
   const int64_t col = k0 + c8 * 8, row = m0 + r8 * 8;
+  const __amdgpu_buffer_rsrc_t x =
+      bytes_rsrc(q.x + m0 * q.ldx, ((min(int64_t(kBlock8), q.M - m0) - 1) * q.ldx + q.K) * 2);
   u32x4 v[8];
-  float a = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (row + i < q.M && col < q.K) v[i] = *reinterpret_cast<const u32x4*>(q.x + (row + i) * q.ldx + col);
+    v[i] = load16(x, uint32_t(r8 * 8 + i) * uint32_t(q.ldx) * 2u + uint32_t(col) * 2u, col < q.K);
   }
+  uint32_t a = finite_abs_max(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_amax8(v[i]));
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
+  for (int s = 32; s > 0; s >>= 1) a = max(a, uint32_t(__shfl_xor(int(a), s)));
   if ((t & 63) == 0) red[t >> 6] = a;
   __syncthreads();
-  const uint32_t byte = exponent_byte(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  const uint32_t byte = exponent_byte(max(max(red[0], red[1]), max(red[2], red[3])));
   u32x2 c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {

@@ -504,10 +504,11 @@ LinearPlan plan_linear(const LinearParams& q) {
 int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
   struct {
     int64_t fixed, slice;
-  } constexpr kCost[] = {{6000, 1400}, {4000, 780}, {3500, 500}, {3000, 370}, {2500, 280}};
+  } constexpr kCost[] = {{6000, 1400}, {5500, 1200}, {4000, 780}, {3500, 500}, {3000, 370}, {2500, 280}};
   int32_t best = 0;
   int64_t best_cost = INT64_MAX;
-  for (int32_t i = 0; i < 5; ++i) {
+  static_assert(sizeof kCost / sizeof *kCost == sizeof kLinear8Tiles / sizeof *kLinear8Tiles, "a cost per tile");
+  for (int32_t i = 0; i < int32_t(sizeof kCost / sizeof *kCost); ++i) {
     const Tile8& t = kLinear8Tiles[i];
     const int64_t tiles = (M + t.bm - 1) / t.bm * ((N + t.bn - 1) / t.bn);
     const int64_t cost = (tiles + kCUs - 1) / kCUs * (kCost[i].fixed + kCost[i].slice * blocks8(K));

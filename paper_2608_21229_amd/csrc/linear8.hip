@@ -16,7 +16,6 @@
 namespace rc {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -76,7 +75,7 @@ __device__ __forceinline__ void store_block(const Linear8Params& q, f32x16 acc, 
 }
 
 template <int ROWS>
-constexpr int kScaleBytes = kScaleSlices * ROWS < 1024 ? 1024 : kScaleSlices * ROWS;
+constexpr int kScaleBytes = (kScaleSlices * ROWS + 1023) / 1024 * 1024;  // whole wave loads
 template <int BM, int BN>
 constexpr int kScaleRing = 2 * (kScaleBytes<BM> + kScaleBytes<BN>);
 
@@ -208,23 +207,26 @@ __global__ __launch_bounds__(WM * WN * 64) void linear8_kernel(const Linear8Para
 // straight into the operands of v_mfma_scale_f32_16x16x128 (lane: row lane % 16, 32
 // of the slice's 128 values), the next slice's loads ahead; the four lanes of a row
 // agree on the block's maximum, and the waves' sums are added in order through LDS.
-constexpr int kFewWaves = 8, kFewTiles = 2;
+constexpr int kFewWaves = 8;
+constexpr int kFewCols = 16 * 256;  // columns up to which 16 per work-group fit one round
 
-template <int MT>
+template <int MT, int NT, int DEPTH>
 __global__ __launch_bounds__(kFewWaves * 64) void linear8_few_kernel(const Linear8Params q) {
-  __shared__ f32x4 sums[kFewWaves][MT][kFewTiles][64];
+  __shared__ f32x4 sums[kFewWaves][MT][NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 15, quarter = lane >> 4;
-  const int n0 = int(blockIdx.x) * 16 * kFewTiles;
+  const int n0 = int(blockIdx.x) * 16 * NT;
   const int64_t m0 = int64_t(blockIdx.y) * 16 * MT;
   const int steps = int(blocks8(q.K));
+  const __amdgpu_buffer_rsrc_t x =
+      bytes_rsrc(q.x + m0 * q.ldx, ((min(int64_t(16 * MT), q.M - m0) - 1) * q.ldx + q.K) * 2);
   struct Slice {
-    u32x4 w[kFewTiles][2], x[MT][4];
-    int ew[kFewTiles];
+    u32x4 w[NT][2], x[MT][4];
+    int ew[NT];
   };
-  const uint8_t *pw[kFewTiles], *pe[kFewTiles];
+  const uint8_t *pw[NT], *pe[NT];
 #pragma unroll
-  for (int t = 0; t < kFewTiles; ++t) {
+  for (int t = 0; t < NT; ++t) {
     const int64_t n = min(n0 + t * 16 + row, q.N - 1);  // columns past the last are not stored
     pw[t] = q.w.codes + n * q.w.ld + quarter * 32;
     pe[t] = q.w.exps + n;
@@ -232,34 +234,31 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear8_few_kernel(const Linea
   const auto load = [&](Slice& z, int s) {
     const int64_t k = int64_t(s) * kBK;
 #pragma unroll
-    for (int t = 0; t < kFewTiles; ++t) {
+    for (int t = 0; t < NT; ++t) {
       z.w[t][0] = *reinterpret_cast<const u32x4*>(pw[t] + k);
       z.w[t][1] = *reinterpret_cast<const u32x4*>(pw[t] + k + 16);
       z.ew[t] = pe[t][s * q.w.le];
     }
 #pragma unroll
     for (int u = 0; u < MT; ++u) {
-      const int64_t m = m0 + u * 16 + row, c = k + quarter * 32;
+      const uint32_t c = uint32_t(k) + quarter * 32, at = uint32_t(u * 16 + row) * uint32_t(q.ldx) * 2u + c * 2u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        z.x[u][i] = u32x4{0u, 0u, 0u, 0u};
-        if (m < q.M && c + 8 * i < q.K) z.x[u][i] = *reinterpret_cast<const u32x4*>(q.x + m * q.ldx + c + 8 * i);
-      }
+      for (int i = 0; i < 4; ++i) z.x[u][i] = load16(x, at + 16 * i, c + 8 * i < uint32_t(q.K));
     }
   };
-  f32x4 acc[MT][kFewTiles];
+  f32x4 acc[MT][NT];
 #pragma unroll
   for (int u = 0; u < MT; ++u)
 #pragma unroll
-    for (int t = 0; t < kFewTiles; ++t) acc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) acc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const auto add = [&](const Slice& z) {
 #pragma unroll
     for (int u = 0; u < MT; ++u) {
-      float a = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a = fmaxf(a, finite_amax8(z.x[u][i]));
-      a = fmaxf(a, __shfl_xor(a, 16));
-      a = fmaxf(a, __shfl_xor(a, 32));
+      uint32_t a = finite_abs_max(z.x[u]);
+      const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+      a = max(r[0], r[1]);
+      const auto h = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+      a = max(h[0], h[1]);
       const uint32_t byte = exponent_byte(a);
       u32x8 fx;
 #pragma unroll
@@ -269,32 +268,32 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear8_few_kernel(const Linea
         fx[2 * i + 1] = c[1];
       }
 #pragma unroll
-      for (int t = 0; t < kFewTiles; ++t) {
+      for (int t = 0; t < NT; ++t) {
         const u32x8 fw = __builtin_shufflevector(z.w[t][0], z.w[t][1], 0, 1, 2, 3, 4, 5, 6, 7);
         acc[u][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
             __builtin_bit_cast(i32x8, fw), __builtin_bit_cast(i32x8, fx), acc[u][t], 0, 0, 0, z.ew[t], 0, int(byte));
       }
     }
   };
-  Slice z0, z1;
+  Slice z[DEPTH];
   int s = wave;
-  if (s < steps) load(z0, s);
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (s + d * kFewWaves < steps) load(z[d], s + d * kFewWaves);
   while (s < steps) {
-    if (s + kFewWaves < steps) load(z1, s + kFewWaves);
-    add(z0);
-    s += kFewWaves;
-    if (s >= steps) break;
-    if (s + kFewWaves < steps) load(z0, s + kFewWaves);
-    add(z1);
-    s += kFewWaves;
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d, s += kFewWaves) {
+      if (s < steps) add(z[d]);
+      if (s + DEPTH * kFewWaves < steps) load(z[d], s + DEPTH * kFewWaves);
+    }
   }
 #pragma unroll
   for (int u = 0; u < MT; ++u)
 #pragma unroll
-    for (int t = 0; t < kFewTiles; ++t) sums[wave][u][t][lane] = acc[u][t];
+    for (int t = 0; t < NT; ++t) sums[wave][u][t][lane] = acc[u][t];
   __syncthreads();
-  for (int i = wave; i < MT * kFewTiles; i += kFewWaves) {
-    const int u = i / kFewTiles, t = i % kFewTiles;
+  for (int i = wave; i < MT * NT; i += kFewWaves) {
+    const int u = i / NT, t = i % NT;
     f32x4 v = sums[0][u][t][lane];
 #pragma unroll
     for (int w = 1; w < kFewWaves; ++w) v += sums[w][u][t][lane];
@@ -326,21 +325,23 @@ int launch_linear8(const Linear8Params& q, int32_t tile, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   switch (tile) {
     case 0: launch_tile<4, 2, 2, 4, 2>(q, s); break;
-    case 1: launch_tile<2, 2, 4, 2, 3>(q, s); break;
-    case 2: launch_tile<2, 2, 2, 2, 4>(q, s); break;
-    case 3: launch_tile<2, 1, 1, 4, 6>(q, s); break;
+    case 1: launch_tile<3, 2, 2, 4, 2>(q, s); break;
+    case 2: launch_tile<2, 2, 4, 2, 3>(q, s); break;
+    case 3: launch_tile<2, 2, 2, 2, 4>(q, s); break;
+    case 4: launch_tile<2, 1, 1, 4, 6>(q, s); break;
     default: launch_tile<1, 1, 2, 2, 8>(q, s); break;
   }
   return int(hipGetLastError());
 }
 
 int launch_linear8_few(const Linear8Params& q, void* stream) {
-  constexpr int kCols = 16 * kFewTiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int mt = q.M <= 16 ? 1 : 2;
-  const dim3 grid((q.N + kCols - 1) / kCols, (q.M + 16 * mt - 1) / (16 * mt)), block(kFewWaves * 64);
-  if (mt == 1) hipLaunchKernelGGL(linear8_few_kernel<1>, grid, block, 0, s, q);
-  else hipLaunchKernelGGL(linear8_few_kernel<2>, grid, block, 0, s, q);
+  const auto launch = [&](auto kernel, int rows, int cols) {
+    hipLaunchKernelGGL(kernel, dim3((q.N + cols - 1) / cols, (q.M + rows - 1) / rows), dim3(kFewWaves * 64), 0, s, q);
+  };
+  if (q.M > 16) launch(linear8_few_kernel<2, 2, 2>, 32, 32);
+  else if (q.N > kFewCols) launch(linear8_few_kernel<1, 2, 3>, 16, 32);
+  else launch(linear8_few_kernel<1, 1, 4>, 16, 16);
   return int(hipGetLastError());
 }
 

@@ -74,11 +74,11 @@ struct WGrad8Params {
 };
 int launch_wgrad8(const WGrad8Params& q, int32_t tile, void* stream) RC_WEAK;
 
-// Products that quantise their bf16 rows themselves, in one launch: up to 16 rows
-// (2 x 7680 x 2560 8.1 us; the quantisation's launch and the product's 4 + 9), or
-// little to read for each group of 32 rows (80 x 384 x 128 in one launch of 4 us
-// instead of two; 32 x 7680 x 2560 14.9 us, as much as both).
-constexpr int64_t kFewRows8 = 16, kFewRead8 = int64_t(4) << 20;
+// Products that quantise their bf16 rows themselves, in one launch: up to 32 rows
+// (2 x 7680 x 2560 6.6 us, 32 rows 11.4; the quantisation's launch and the product's
+// 4 + 9.5 and the host's time for a second launch), or little to read for each
+// group of 32 rows (80 x 384 x 128 3.6 us, as much as the quantisation alone).
+constexpr int64_t kFewRows8 = 32, kFewRead8 = int64_t(4) << 20;
 constexpr bool few_rows8(int64_t M, int32_t N, int32_t K) {
   return M <= kFewRows8 || (M + 31) / 32 * N * pad8(K) <= kFewRead8;
 }
@@ -86,7 +86,7 @@ constexpr bool few_rows8(int64_t M, int32_t N, int32_t K) {
 struct Tile8 {
   int32_t bm, bn;
 };
-constexpr Tile8 kLinear8Tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 128}, {64, 64}};
+constexpr Tile8 kLinear8Tiles[] = {{256, 256}, {192, 256}, {256, 128}, {128, 128}, {64, 128}, {64, 64}};
 int32_t plan_linear8(int64_t M, int32_t N, int32_t K);
 
 constexpr Tile8 kWGrad8Tiles[] = {{256, 256}, {256, 128}, {128, 128}};  // n x k

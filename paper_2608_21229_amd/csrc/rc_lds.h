@@ -1,7 +1,9 @@
-// Tiles in LDS: direct loads, barriers, the order of work-groups.
+// Loads by buffer descriptor, tiles in LDS, barriers, the order of work-groups.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "rc_device.h"
 
 namespace rc {
 
@@ -22,6 +24,12 @@ __device__ __forceinline__ void dma16(uint32_t lds, uint32_t voff, __amdgpu_buff
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_rsrc(const void* p, int64_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, int(bytes), 0x00020000);
+}
+
+// 16 bytes; zeros past the record count, and where `in` is false.  Without a branch, so
+// that many are in flight.
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off, bool in) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, int(in ? off : 0xfffffff0u), 0, 0);
 }
 
 // Barrier that waits for this wave's LDS accesses but not for its loads in flight.

@@ -54,7 +54,7 @@ def test_random_calls():
         need = rc.lib().rc_linear_fp8_backward_workspace_bytes(M, N, K, 0, 1)
         stub("workspace", WS, need)
         assert back(M=M, N=N, K=K, lddy=N, dx=None, w_t=None, lddw=K, ws=WS, wsb=need) == rc.RC_OK
-    assert seen == {0, 1, 2, 3, 4} and few > 40 and split > 100 and whole > 2
+    assert seen == {0, 1, 2, 3, 4, 5} and few > 40 and split > 100 and whole > 2
 
 
 def test_limits_of_the_grid():

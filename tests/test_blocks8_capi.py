@@ -99,8 +99,8 @@ def test_product_workspace():
     need = rc.lib().rc_linear_fp8_workspace_bytes
     assert need(1000, 4096, 4096) == 1000 * 4096 + 32 * 1008
     assert need(1000, 4096, 4104) == 1000 * 4224 + 33 * 1008
-    assert need(16, 1 << 20, 1 << 20) == 0 and need(80, 384, 128) == 0 and need(0, 8, 8) == 0
-    assert need(17, 7680, 2560) > 0
+    assert need(32, 1 << 20, 1 << 20) == 0 and need(80, 384, 128) == 0 and need(0, 8, 8) == 0
+    assert need(33, 7680, 2560) > 0
     assert need(-1, 8, 8) == need(8, 9, 8) == need(8, 8, 0) == 0
 
 

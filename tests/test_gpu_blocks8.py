@@ -93,8 +93,32 @@ def test_quantize_extremes():
     assert back[4, 1] == 2.0 and back[5, 1] == -3.0 and back[1, 5] == 2.0 ** -133
 
 
-LINEAR = [(1, 8, 8), (1, 128, 128), (2, 2560, 1032), (16, 72, 640), (17, 384, 128), (80, 384, 128), (65, 264, 520),
-          (128, 128, 2560), (129, 1032, 1160), (300, 2568, 264), (1025, 640, 1288)]
+def test_quantize_every_value():
+    """Every bf16 value beside its neighbours, and beside larger ones up to the largest
+    for which it is not rounded to zero."""
+    bits = torch.arange(1 << 15, dtype=torch.int32)
+    signs = torch.stack([bits, bits + (1 << 15)], 1).view(-1, 128)   # 64 neighbours of both signs
+    rows = [signs]
+    for up in (1, 3, 6, 9, 14, 18):                                   # 2^up times the neighbours'
+        r = signs.clone()
+        r[:, 0] = (r[:, -1] + (up << 7)) & 0x7fff
+        rows.append(r)
+    x = torch.cat(rows).to(torch.int16).view(torch.bfloat16)
+    b = rc.quantize_blocks(x.cuda())
+    codes, exps, _ = plain.quantize(x)
+    assert torch.equal(plain.exps_of(b), exps)
+    assert torch.equal(plain.codes_of(b).nan_to_num(999.0), codes.nan_to_num(999.0))
+    # the same on a product's way: times one
+    w8 = rc.quantize_blocks(torch.eye(128, dtype=torch.bfloat16).cuda(), square=True)
+    few = torch.cat([rc.linear_fp8(x[i:i + 16].cuda(), w8) for i in range(0, 512, 16)]).cpu()
+    want = rc.dequantize_blocks(b)[:512].cpu()
+    bad = x[:512].float().isfinite().logical_not().any(1)
+    assert torch.equal(few[~bad], want[~bad])
+
+
+# one launch for up to 32 rows and for the small ones; 16 or 32 columns per work-group
+LINEAR = [(1, 8, 8), (1, 128, 128), (2, 2560, 1032), (2, 4104, 520), (16, 72, 640), (17, 384, 128), (31, 4168, 1288),
+          (80, 384, 128), (65, 264, 520), (128, 128, 2560), (129, 1032, 1160), (300, 2568, 264), (1025, 640, 1288)]
 
 
 @pytest.mark.parametrize("m,n,k", LINEAR)
@@ -120,8 +144,10 @@ def test_linear_row_blocks_on_both_sides():
     near(rc.linear_fp8(x, rc.quantize_blocks(w)), want, size, adds8(520), 2.0 ** -8, cut)
 
 
-# one of every tile size, by rounds of 256 work-groups
-@pytest.mark.parametrize("m,n,k", [(4096, 4096, 256), (4096, 2048, 384), (2000, 2048, 256), (900, 2048, 128)])
+# each of the tile sizes, by rounds of 256 work-groups; inner lengths of one and of several scale loads (1024 each)
+@pytest.mark.parametrize("m,n,k", [(4096, 4096, 256), (4096, 4096, 2312), (4315, 2560, 520), (4315, 2560, 2568),
+                                   (4096, 2048, 384), (4096, 2048, 2568), (2000, 2048, 256), (2000, 2048, 2312), (1500, 1280, 264),
+                                   (1500, 1280, 2696), (900, 2048, 128), (900, 2048, 2304), (200, 2048, 640), (200, 2048, 2440)])
 def test_linear_tiles(m, n, k):
     g = torch.Generator(device="cuda").manual_seed(m)
     x = torch.randn(m, k, generator=g, device="cuda").bfloat16()
@@ -140,7 +166,7 @@ def test_linear_rows_do_not_depend_on_each_other():
     whole = rc.linear_fp8(rc.quantize_blocks(x), w8)
     for at, n in ((0, 1), (7, 40), (100, 700), (3000, 2000)):
         assert torch.equal(rc.linear_fp8(rc.quantize_blocks(x[at:at + n]), w8), whole[at:at + n])
-        if n > 16:
+        if n > 32:
             assert torch.equal(rc.linear_fp8(x[at:at + n], w8), whole[at:at + n])
 
 
