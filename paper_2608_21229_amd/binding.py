@@ -628,12 +628,7 @@ def dequantize_blocks(x, out=None, stream=None):
     """The values of Fp8Blocks in bf16 [M, K] (exact).  Returns out."""
     M, K = _blocks(x, "x")
     dev = x.device
-    if out is None:
-        out = _empty((M, K), _torch().bfloat16, dev, stream)
-    elif out.shape != (M, K):
-        raise ValueError(f"out must have shape {(M, K)}, got {tuple(out.shape)}")
-    ldo = _rows_view(out, "out")
-    _same_device(dev, out=out)
+    out, ldo = _rows_out(out, "out", M, K, dev, stream)
     _call(lib().rc_dequantize_blocks, dev, stream, M, K, ctypes.byref(x.c), out.data_ptr(), ldo)
     return out
 
@@ -645,29 +640,42 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     stride; out may be residual).  A row's result does not depend on M for
     Fp8Blocks; a small bf16 call (up to 32 rows, or little work) sums in another order.
     Returns out."""
-    torch, L = _torch(), lib()
-    blocks = isinstance(a, Fp8Blocks)
+    L, blocks = lib(), isinstance(a, Fp8Blocks)
     lda = 0 if blocks else _rows_view(a, "a")
     M, K = _blocks(a, "a") if blocks else a.shape
-    dev = a.device
-    N = _blocks(w, "w", cols=K)[0]
-    if out is None:
-        out = _empty((M, N), torch.bfloat16, dev, stream)
-    for name, t in (("out", out), ("residual", residual)):
-        if t is not None and t.shape != (M, N):
-            raise ValueError(f"{name} must have shape {(M, N)}, got {tuple(t.shape)}")
-    ldo = _rows_view(out, "out")
-    ldr = _rows_view(residual, "residual") if residual is not None else 0
-    _same_device(dev, w=w, out=out, residual=residual)
+    dev, N = a.device, _blocks(w, "w", cols=K)[0]
+    out, ldo = _rows_out(out, "out", M, N, dev, stream)
+    ldr = _rows_in(residual, "residual", M, N, dev)
+    if w.device != dev:
+        raise ValueError(f"w is on {w.device}, the inputs on {dev}")
     if blocks:
         _call(L.rc_linear_fp8_blocks, dev, stream, M, N, K, ctypes.byref(a.c), ctypes.byref(w.c), _ptr(residual), ldr,
               out.data_ptr(), ldo)
         return out
     need = L.rc_linear_fp8_workspace_bytes(M, N, K)
-    workspace = _workspace(workspace, need, dev, stream)
+    workspace = _workspace(workspace, need, dev, stream) if need else None
     _call(L.rc_linear_fp8, dev, stream, M, N, K, a.data_ptr(), lda, ctypes.byref(w.c), _ptr(residual), ldr,
           out.data_ptr(), ldo, _ptr(workspace), need)
     return out
+
+
+def _rows_out(t, what, rows, cols, dev, stream):
+    """A bf16 output [rows, cols] and its row stride: the caller's, or new memory, which needs no checks."""
+    if t is None:
+        return _empty((rows, cols), _torch().bfloat16, dev, stream), cols
+    return t, _rows_in(t, what, rows, cols, dev)
+
+
+def _rows_in(t, what, rows, cols, dev):
+    """The row stride of a checked bf16 [rows, cols] tensor; 0 for None."""
+    if t is None:
+        return 0
+    if t.shape != (rows, cols):
+        raise ValueError(f"{what} must have shape {(rows, cols)}, got {tuple(t.shape)}")
+    ld = _rows_view(t, what)
+    if t.device != dev:
+        raise ValueError(f"{what} is on {t.device}, the inputs on {dev}")
+    return ld
 
 
 def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True, want_dw=True, workspace=None,
@@ -677,8 +685,7 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row;
     dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual.  Returns (dx, dw), None
     for what is not wanted (x and w may then be None)."""
-    torch, L = _torch(), lib()
-    lddy = _rows_view(dy, "dy")
+    L, lddy, lddx, ldr, w_t = lib(), _rows_view(dy, "dy"), 0, 0, None
     dev = dy.device
     M, N = dy.shape
     if not (want_dx or want_dw):
@@ -688,27 +695,23 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     if (dx is not None and not want_dx) or (dw is not None and not want_dw):
         raise ValueError("dx or dw is given but not wanted")
     K = (_blocks(w, "w", rows=N) if want_dx else _blocks(x, "x", rows=M))[1]
-    w_t = None
     if want_dx:
-        if w.t is None:
-            raise ValueError("w has no transposed form: quantize_blocks(w, square=True, transposed=True)")
         w_t = w.t
+        if w_t is None:
+            raise ValueError("w has no transposed form: quantize_blocks(w, square=True, transposed=True)")
         _blocks(w_t, "w.t", K, N)
-        if dx is None:
-            dx = _empty((M, K), torch.bfloat16, dev, stream)
-        for name, t in (("dx", dx), ("residual", residual)):
-            if t is not None and t.shape != (M, K):
-                raise ValueError(f"{name} must have shape {(M, K)}, got {tuple(t.shape)}")
+        dx, lddx = _rows_out(dx, "dx", M, K, dev, stream)
+        ldr = _rows_in(residual, "residual", M, K, dev)
     if want_dw:
         _blocks(x, "x", M, K)
         if dw is None:
-            dw = _empty((N, K), torch.float32, dev, stream)
-        _expect(dw, (N, K), "torch.float32", "dw")
-    lddx = _rows_view(dx, "dx") if want_dx else 0
-    ldr = _rows_view(residual, "residual") if residual is not None else 0
-    _same_device(dev, dx=dx, dw=dw, residual=residual, x=x if want_dw else None, w=w_t)
+            dw = _empty((N, K), _torch().float32, dev, stream)
+        else:
+            _expect(dw, (N, K), "torch.float32", "dw")
+            _same_device(dev, dw=dw)
+    _same_device(dev, x=x if want_dw else None, w=w_t)
     need = L.rc_linear_fp8_backward_workspace_bytes(M, N, K, int(want_dx), int(want_dw))
-    workspace = _workspace(workspace, need, dev, stream)
+    workspace = _workspace(workspace, need, dev, stream) if need else None
     _call(L.rc_linear_fp8_backward, dev, stream, M, N, K, dy.data_ptr(), lddy, ctypes.byref(x.c) if want_dw else None,
           ctypes.byref(w_t.c) if want_dx else None, _ptr(residual), ldr, _ptr(dx), lddx, _ptr(dw), K, _ptr(workspace), need)
     return dx, dw
@@ -716,8 +719,6 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
 
 def _workspace(workspace, need, dev, stream):
     """The caller's workspace where it is large enough, else one of this call's."""
-    if not need:
-        return None
     if workspace is None or workspace.numel() * workspace.element_size() < need:
         return _empty(need, _torch().uint8, dev, stream, returned=False)
     _same_device(dev, workspace=workspace)

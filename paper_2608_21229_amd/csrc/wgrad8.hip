@@ -34,15 +34,17 @@ __device__ __forceinline__ int swz(int row) { return (row & 3) << 2 | (row >> 2 
 // Shares of the same rows are neighbours on one XCD: they read the same dy and x
 // from its L2 (250 shares in another order were bound by 7.8 TB/s of them).
 //
-// Two stages of 64 rows of both operands.  A wave runs one stream of matrix
-// instructions; between them, in an order fixed by scheduling fences, go the
-// fragment reads of the next 16 rows, the widening of the next slice's codes
-// (loaded into registers a slice ago, then reloaded) and the direct loads of dy.
-// The one barrier per slice lies before its last 16 rows, whose fragments are in
-// registers by then: behind it the next slice's first fragments are read and its
-// successor's dy is loaded into the stage that has just been read.  Slices past
-// the share's last one load zeros, so the loop has no other branch.
-template <int NB, int KB, int WN, int WK>
+// A ring of ST stages of 64 rows of both operands.  A wave runs one stream of
+// matrix instructions; between them, in an order fixed by scheduling fences, go
+// the fragment reads of the next 16 rows, the widening of the next slice's codes
+// (loaded into one of XD sets of registers XD slices ago, then reloaded) and the
+// direct loads of dy.  The one barrier per slice lies before its last 16 rows,
+// whose fragments are in registers by then: behind it the next slice's first
+// fragments are read, and dy of the slice ST further is loaded into the stage that
+// has just been read.  A smaller tile has less time per slice, so its loads go out
+// more slices ahead.  Slices past the share's last one load zeros, so the loop has
+// no other branch, and runs a multiple of XD slices.
+template <int NB, int KB, int WN, int WK, int ST, int XD>
 __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void wgrad8_kernel(
     const WGrad8Params q) {
   constexpr int NW = WN * WK;
@@ -54,7 +56,7 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
   constexpr int IX = RQ * GX / (NW * 64);        // groups per thread
   constexpr int NX = IX * 4;                     // granules per thread
   static_assert(CD * NW * 1024 == kDy && IX * NW * 64 == RQ * GX && NW * 64 % GX == 0, "loads divide over the waves");
-  __shared__ __attribute__((aligned(1024))) char ring[2 * kStage];
+  __shared__ __attribute__((aligned(1024))) char ring[ST * kStage];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave / WK, wk = wave % WK;
@@ -98,27 +100,27 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
   constexpr int kRowStep = NW * 64 / GX * 4;  // rows between a thread's groups
   const int kblocks = int(blocks8(q.K)), kb0 = k0 / kBlock8;
   const int dkb = min(gx * 8 / kBlock8, kblocks - 1 - kb0);
-  u32x2 xc[NX];
-  uint32_t xe[IX], xe_now = 0;
+  u32x2 xc[XD][NX];
+  uint32_t xe[XD][IX], xe_now = 0;
   int xoff[NX], eoff[IX];
 #pragma unroll
   for (int j = 0; j < NX; ++j) xoff[j] = (xrow + j / 4 * kRowStep + j % 4) * int(q.x.ld) + gx * 8;
 #pragma unroll
   for (int i = 0; i < IX; ++i) eoff[i] = int(uint32_t(dkb) * uint32_t(q.x.le)) + xrow + i * kRowStep;
-  const auto load_codes = [&](__amdgpu_buffer_rsrc_t r, int j) {
-    xc[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, xoff[j], 0, 0));
+  const auto load_codes = [&](int set, __amdgpu_buffer_rsrc_t r, int j) {
+    xc[set][j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, xoff[j], 0, 0));
   };
-  const auto load_exps = [&](__amdgpu_buffer_rsrc_t r, int i) {
-    xe[i] = __builtin_amdgcn_raw_buffer_load_b32(r, eoff[i], 0, 0);
+  const auto load_exps = [&](int set, __amdgpu_buffer_rsrc_t r, int i) {
+    xe[set][i] = __builtin_amdgcn_raw_buffer_load_b32(r, eoff[i], 0, 0);
   };
   static_assert(kRowStep % 16 == 0, "a thread's groups have one swizzle");
   uint32_t xlds[4];  // where the granules of a group go
 #pragma unroll
   for (int j = 0; j < 4; ++j) xlds[j] = uint32_t(kDy + (xrow + j) * TK * 2 + 16 * (gx ^ swz(xrow + j)));
   // granule j with the exponents of its group in xe_now
-  const auto widen = [&](uint32_t stage, int j) {
+  const auto widen = [&](int set, uint32_t stage, int j) {
     *reinterpret_cast<u32x4*>(ring + stage + xlds[j % 4] + j / 4 * kRowStep * TK * 2) =
-        values8_any(xc[j], xe_now >> (8 * (j % 4)));
+        values8_any(xc[set][j], xe_now >> (8 * (j % 4)));
   };
 
   // The streams of slices: where the next one starts and the share's rows from
@@ -183,37 +185,40 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
+  constexpr int kNewer = (ST - 2) * (CD + NX + IX) + NX + IX;  // loads behind those of the next slice's dy
+  static_assert(kNewer <= 63, "vmcnt range");
   const int n_slices = int(s1 - s0);
   __amdgpu_buffer_rsrc_t r_codes, r_exps;
   if (n_slices > 0) {
-    const __amdgpu_buffer_rsrc_t first = next_dy();
-#pragma unroll
-    for (int i = 0; i < CD; ++i) issue_dy(0, first, i);
     // in the order in which the loop reloads them
-    const auto load_x = [&] {
+    const auto load_x = [&](int set) {
       r_codes = next_codes();
       r_exps = next_exps();
 #pragma unroll
       for (int j = 0; j < NX; ++j) {
-        if (j % 4 == 0) load_exps(r_exps, j / 4);
+        if (j % 4 == 0) load_exps(set, r_exps, j / 4);
         sched_fence();
-        load_codes(r_codes, j);
+        load_codes(set, r_codes, j);
         sched_fence();
       }
     };
-    load_x();
-    const __amdgpu_buffer_rsrc_t second = next_dy();
+    load_x(0);
 #pragma unroll
-    for (int i = 0; i < CD; ++i) issue_dy(kStage, second, i);
+    for (int s = 0; s < ST; ++s) {
+      const __amdgpu_buffer_rsrc_t r = next_dy();
+#pragma unroll
+      for (int i = 0; i < CD; ++i) issue_dy(s * kStage, r, i);
+    }
 #pragma unroll
     for (int j = 0; j < NX; ++j) {
-      xe_now = xe[j / 4];
-      widen(0, j);
+      xe_now = xe[0][j / 4];
+      widen(0, 0, j);
     }
-    load_x();
+#pragma unroll
+    for (int x = 1; x <= XD; ++x) load_x(x % XD);
     r_codes = next_codes();
     r_exps = next_exps();
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NX + IX) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(XD * (NX + IX)) : "memory");
     lds_barrier();
 #pragma unroll
     for (int t = 0; t < NF; ++t)
@@ -221,14 +226,15 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
       for (int h = 0; h < 2; ++h) read(0, t, h);
   }
   uint32_t cur = 0;
-  for (int s = 0; s < n_slices; ++s) {
-    const uint32_t next = kStage - cur;
+  // slice s, whose successor's codes are in `set`
+  const auto slice = [&](int set) {
+    const uint32_t next = cur + kStage == ST * kStage ? 0 : cur + kStage;
     __amdgpu_buffer_rsrc_t r_dy;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       if (c == 3) {
-        // dy of the next slice has landed (only the codes' loads are newer), its x is written
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NX + IX) : "memory");
+        // dy of the next slice has landed, its x is written
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kNewer) : "memory");
         lds_barrier();
       }
 #pragma unroll
@@ -253,11 +259,11 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
           for (int j = 0; j < NX; ++j)
             if (j * 3 * NM / NX == c * NM + t) {
               if (j % 4 == 0) {
-                xe_now = xe[j / 4];
-                load_exps(r_exps, j / 4);
+                xe_now = xe[set][j / 4];
+                load_exps(set, r_exps, j / 4);
               }
-              widen(next, j);
-              load_codes(r_codes, j);
+              widen(set, next, j);
+              load_codes(set, r_codes, j);
             }
           if (c == 2 && t == NM - 1) r_dy = next_dy();
         }
@@ -265,7 +271,10 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
       }
     }
     cur = next;
-  }
+  };
+  for (int s = 0; s < n_slices; s += XD)
+#pragma unroll
+    for (int x = 1; x <= XD; ++x) slice(x % XD);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the work-group
 
   if (share >= 0 && q.splits > 1) {
@@ -320,11 +329,11 @@ __global__ __launch_bounds__(WN * WK * 64) void wgrad8_join_kernel(const WGrad8P
     if (n < q.N && k + 8 * r < q.K) *reinterpret_cast<f32x4*>(q.dw + n * q.lddw + k + 8 * r) = v[r];
 }
 
-template <int NB, int KB, int WN, int WK>
+template <int NB, int KB, int WN, int WK, int ST, int XD>
 void launch_tile(const WGrad8Params& q, hipStream_t s) {
   constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK;
   const int64_t rest = int64_t((q.N + TN - 1) / TN) * ((q.K + TK - 1) / TK) - q.whole;
-  hipLaunchKernelGGL((wgrad8_kernel<NB, KB, WN, WK>), dim3(q.whole + rest * q.splits), dim3(WN * WK * 64), 0, s, q);
+  hipLaunchKernelGGL((wgrad8_kernel<NB, KB, WN, WK, ST, XD>), dim3(q.whole + rest * q.splits), dim3(WN * WK * 64), 0, s, q);
   if (q.splits > 1)
     hipLaunchKernelGGL((wgrad8_join_kernel<NB, KB, WN, WK>), dim3(rest * NB * KB), dim3(WN * WK * 64), 0, s, q);
 }
@@ -334,9 +343,9 @@ void launch_tile(const WGrad8Params& q, hipStream_t s) {
 int launch_wgrad8(const WGrad8Params& q, int32_t tile, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   switch (tile) {
-    case 0: launch_tile<4, 4, 2, 2>(q, s); break;
-    case 1: launch_tile<4, 2, 2, 2>(q, s); break;
-    default: launch_tile<2, 2, 2, 2>(q, s); break;
+    case 0: launch_tile<4, 4, 2, 2, 2, 1>(q, s); break;
+    case 1: launch_tile<4, 2, 2, 2, 3, 2>(q, s); break;
+    default: launch_tile<2, 2, 2, 2, 4, 2>(q, s); break;
   }
   return int(hipGetLastError());
 }
