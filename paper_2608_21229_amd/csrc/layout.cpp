@@ -525,7 +525,7 @@ int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
 WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K) {
   struct {
     int64_t fixed, slice;
-  } constexpr kCost[] = {{5500, 1300}, {5000, 930}, {4000, 690}};
+  } constexpr kCost[] = {{5500, 1250}, {5000, 800}, {4000, 620}};
   const int64_t slices = (M + 63) / 64;
   WGrad8Plan best{0, 1, 0, 0};
   int64_t best_cost = INT64_MAX;
@@ -539,7 +539,7 @@ WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K) {
       const int64_t bytes = int64_t(t.bm) * t.bn * 4, rate = 5000;  // of a tile; bytes per ns
       int64_t cost = whole / kCUs * (c.fixed + slices * c.slice + kCUs * bytes / rate);
       if (rest > 0) cost += c.fixed + (slices + j - 1) / j * c.slice + j * rest * bytes / rate;
-      if (j > 1) cost += 4000 + j * rest * bytes / rate;  // the join
+      if (j > 1) cost += 4000 + 130 * j + j * rest * bytes / rate;  // the join
       if (cost < best_cost) {
         best_cost = cost;
         best = WGrad8Plan{i, int32_t(j), whole, tiles};

@@ -75,14 +75,16 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t amax) {
 // The scale as the conversions take it: they read its exponent field.
 __device__ __forceinline__ float scale8(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-__device__ __forceinline__ u32x4 scaled_values8(u32x2 c, float s) {
-  u32x4 out;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    out[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, false));
-    out[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, true));
-  }
-  return out;
+// Of the low byte of any bits: finite whatever lies in place of the exponent, 255 (a
+// scale of no number, which no block has) included, so that zeros stay zeros.
+__device__ __forceinline__ float scale8_any(uint32_t bits) {
+  return __uint_as_float(min(bits << 23 & 0x7f800000u, 0x7f000000u));
+}
+
+// The low or high two of four codes times the scale, in bf16.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t widened(uint32_t codes, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s, HIGH));
 }
 
 // Codes of 8 bf16 values: the conversion takes 2^e out exactly, rounds to nearest
@@ -99,12 +101,9 @@ __device__ __forceinline__ u32x2 codes8(u32x4 g, uint32_t byte) {
 }
 
 // 8 codes times 2^e in bf16.
-__device__ __forceinline__ u32x4 values8(u32x2 c, uint32_t byte) { return scaled_values8(c, scale8(byte)); }
-
-// The same for the low byte of any bits: zeros stay zeros whatever lies in place
-// of their exponent, 255 (a scale of no number, which no block has) included.
-__device__ __forceinline__ u32x4 values8_any(u32x2 c, uint32_t bits) {
-  return scaled_values8(c, __uint_as_float(min(bits << 23 & 0x7f800000u, 0x7f000000u)));
+__device__ __forceinline__ u32x4 values8(u32x2 c, uint32_t byte) {
+  const float s = scale8(byte);
+  return u32x4{widened<false>(c[0], s), widened<true>(c[0], s), widened<false>(c[1], s), widened<true>(c[1], s)};
 }
 
 }  // namespace rc

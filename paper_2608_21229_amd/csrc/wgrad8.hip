@@ -2,12 +2,13 @@
 //
 //   dw[n, k] = sum_m dy[m, n] x[m, k],  x = code 2^e, dy in bf16, fp32 sums and result
 //
-// The codes are widened to bf16 (exact) on their way into LDS, so the product is
-// one of v_mfma_f32_32x32x16_bf16.  The sum runs over rows, which both operands
-// hold as their slow dimension: the fragments are read with the transpose read
-// ds_read_b64_tr_b16 (16 lanes take 4 rows of 16 columns, each lane a column).
+// The codes are widened to bf16 (exact), so the product is one of
+// v_mfma_f32_32x32x16_bf16.  The sum runs over rows, which both operands hold as
+// their slow dimension; they are transposed in registers on their way into LDS.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "rc_blocks8.h"
 #include "rc_lds.h"
@@ -16,47 +17,62 @@
 namespace rc {
 namespace {
 
-typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef const __attribute__((address_space(3))) bf16x8 lds_cbf16x8;
 
 constexpr int kSlice = 64;  // rows per step
 
-// Granule g (8 columns) of row r lies at slot g ^ swz(r): the four rows of a
-// transpose read fall into four quarters of the banks.
-__device__ __forceinline__ int swz(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
+// LDS holds a slice's columns as rows of 64 values (128 bytes); the 16 bytes of 8
+// rows g of column c lie at part g ^ part8(c): the writes, of columns 4 or 8 apart,
+// and the reads, of neighbouring columns, both meet every bank once.
+__device__ __forceinline__ int part8(int c) { return (c ^ c >> 3) & 7; }
+
+// 4 or 8 columns of 8 rows, as loaded: row r's are in d[r].
+template <int P>
+struct Block {
+  uint32_t d[8][P / 4];  // codes
+};
+template <int P>
+struct BlockBf16 {
+  uint32_t d[8][P / 2];
+};
+
+// The 16 bytes of column 2 p (or 2 p + 1) of 8 rows, of whose dwords each holds both.
+template <bool ODD>
+__device__ __forceinline__ u32x4 column(const uint32_t (&r)[8]) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], ODD ? 0x07060302u : 0x05040100u);
+  return v;
+}
 
 // Tiles of n x k: WN x WK waves, each NB x KB accumulators of 32 x 32, one wave
 // per SIMD.  The first `whole` work-groups take a tile each, with all rows; the
 // remaining tiles, less than a round of the CUs, are cut into `splits` shares of
 // their rows, whose sums go to the workspace and are added in order by the join.
 // Shares of the same rows are neighbours on one XCD: they read the same dy and x
-// from its L2 (250 shares in another order were bound by 7.8 TB/s of them).
+// from its L2.
 //
-// A ring of ST stages of 64 rows of both operands.  A wave runs one stream of
-// matrix instructions; between them, in an order fixed by scheduling fences, go
-// the fragment reads of the next 16 rows, the widening of the next slice's codes
-// (loaded into one of XD sets of registers XD slices ago, then reloaded) and the
-// direct loads of dy.  The one barrier per slice lies before its last 16 rows,
-// whose fragments are in registers by then: behind it the next slice's first
-// fragments are read, and dy of the slice ST further is loaded into the stage that
-// has just been read.  A smaller tile has less time per slice, so its loads go out
-// more slices ahead.  Slices past the share's last one load zeros, so the loop has
-// no other branch, and runs a multiple of XD slices.
-template <int NB, int KB, int WN, int WK, int ST, int XD>
-__global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void wgrad8_kernel(
-    const WGrad8Params q) {
-  constexpr int NW = WN * WK;
-  constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK;
+// Two stages of 64 rows of both operands.  A wave runs one stream of matrix
+// instructions; between them, in an order fixed by scheduling fences, go the
+// fragment reads of the next 16 rows and the way of the slices ahead: a thread
+// holds 8 rows of 4 or 8 columns of each operand in registers, widens and transposes
+// them into the stage that is free, and loads the next slice's.  The one barrier per
+// slice lies before its last 16 rows, whose fragments are in registers by then:
+// behind it the next slice's first fragments are read, and its own stage is written
+// again.  Slices past the share's last one load zeros, so the loop has no other branch.
+//
+// What bounds it: 64 products of 32 cycles per slice and SIMD (256 x 256), beside
+// 1 536 cycles of LDS.  (With dy loaded straight into LDS, and both operands read by
+// the transpose read ds_read_b64_tr_b16, which takes twice the cycles per byte, LDS
+// was busy 2 560 cycles and the slice took as long.)
+template <int NB, int KB, int WN, int WK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void wgrad8_kernel(const WGrad8Params q) {
+  static_assert(WN * WK == 4, "four waves");
+  constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK, PN = TN / 32, PK = TK / 32;
   constexpr int kDy = kSlice * TN * 2, kX = kSlice * TK * 2, kStage = kDy + kX;
-  constexpr int CD = kDy / 1024 / NW;            // 1 KB chunks of dy per wave
-  constexpr int GX = TK / 8;                     // granules of a row of x
-  constexpr int RQ = kSlice / 4;                 // groups of four rows
-  constexpr int IX = RQ * GX / (NW * 64);        // groups per thread
-  constexpr int NX = IX * 4;                     // granules per thread
-  static_assert(CD * NW * 1024 == kDy && IX * NW * 64 == RQ * GX && NW * 64 % GX == 0, "loads divide over the waves");
-  __shared__ __attribute__((aligned(1024))) char ring[ST * kStage];
+  __shared__ __attribute__((aligned(1024))) char ring[2 * kStage];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave / WK, wk = wave % WK;
@@ -81,52 +97,14 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
     s1 = slices * (split + 1) / q.splits;
   }
 
-  // dy: lane l of chunk c fills slot 64 c + l
-  constexpr int GD = TN / 8;
-  uint32_t doff[CD];
-#pragma unroll
-  for (int i = 0; i < CD; ++i) {
-    const int p = (i * NW + wave) * 64 + lane, row = p / GD;
-    doff[i] = uint32_t(row) * uint32_t(q.lddy) * 2u + uint32_t((p % GD) ^ swz(row)) * 16u;
-  }
-  const uint32_t lds0 = lds_u32(ring);
-  const auto issue_dy = [&](uint32_t stage, __amdgpu_buffer_rsrc_t r, int i) {
-    dma16(lds0 + stage + uint32_t((i * NW + wave) * 1024), doff[i], r);
-  };
-
-  // x: a thread takes 8 codes of four consecutive rows, whose exponents are one
-  // dword, IX times; granule j of a slice is in xc[j]
-  const int gx = tid % GX, xrow = tid / GX * 4;
-  constexpr int kRowStep = NW * 64 / GX * 4;  // rows between a thread's groups
+  // This thread's 8 rows and its columns of both operands.
+  const int col = tid & 31, row8 = tid >> 5;
   const int kblocks = int(blocks8(q.K)), kb0 = k0 / kBlock8;
-  const int dkb = min(gx * 8 / kBlock8, kblocks - 1 - kb0);
-  u32x2 xc[XD][NX];
-  uint32_t xe[XD][IX], xe_now = 0;
-  int xoff[NX], eoff[IX];
-#pragma unroll
-  for (int j = 0; j < NX; ++j) xoff[j] = (xrow + j / 4 * kRowStep + j % 4) * int(q.x.ld) + gx * 8;
-#pragma unroll
-  for (int i = 0; i < IX; ++i) eoff[i] = int(uint32_t(dkb) * uint32_t(q.x.le)) + xrow + i * kRowStep;
-  const auto load_codes = [&](int set, __amdgpu_buffer_rsrc_t r, int j) {
-    xc[set][j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, xoff[j], 0, 0));
-  };
-  const auto load_exps = [&](int set, __amdgpu_buffer_rsrc_t r, int i) {
-    xe[set][i] = __builtin_amdgcn_raw_buffer_load_b32(r, eoff[i], 0, 0);
-  };
-  static_assert(kRowStep % 16 == 0, "a thread's groups have one swizzle");
-  uint32_t xlds[4];  // where the granules of a group go
-#pragma unroll
-  for (int j = 0; j < 4; ++j) xlds[j] = uint32_t(kDy + (xrow + j) * TK * 2 + 16 * (gx ^ swz(xrow + j)));
-  // granule j with the exponents of its group in xe_now
-  const auto widen = [&](int set, uint32_t stage, int j) {
-    *reinterpret_cast<u32x4*>(ring + stage + xlds[j % 4] + j / 4 * kRowStep * TK * 2) =
-        values8_any(xc[set][j], xe_now >> (8 * (j % 4)));
-  };
-
-  // The streams of slices: where the next one starts and the share's rows from
-  // there on.  Loads past the rows (and of slices past the last) give zeros.
+  const int dkb = min(col * PK / kBlock8, kblocks - 1 - kb0);
   const int64_t m0 = s0 * kSlice;
   const int rows = int(min(s1 * kSlice, q.M) - m0);
+  // The streams of slices: where the next one starts and the share's rows from
+  // there on.  Loads past the rows (and of slices past the last) give zeros.
   const char* dy_at = reinterpret_cast<const char*>(q.dy + m0 * q.lddy + n0);
   const uint8_t* codes_at = q.x.codes + m0 * q.x.ld + k0;
   const uint8_t* exps_at = q.x.exps + kb0 * q.x.le + m0;
@@ -134,47 +112,95 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
   const int dy_cols = min(TN, q.N - n0) * 2, x_cols = min(TK, kblocks * kBlock8 - k0);
   const int dy_ld = int(q.lddy) * 2, x_ld = int(q.x.ld);
   const int64_t exps_more = (kblocks - kb0) * q.x.le - m0;
-  const auto next_dy = [&] {
-    const __amdgpu_buffer_rsrc_t r = bytes_rsrc(dy_at, dy_left > 0 ? (min(kSlice, dy_left) - 1) * dy_ld + dy_cols : 0);
-    dy_at += kSlice * dy_ld;
-    dy_left -= kSlice;
-    return r;
-  };
-  // the codes' descriptor, then the exponents'
-  const auto next_codes = [&] {
-    return bytes_rsrc(codes_at, codes_left > 0 ? (min(kSlice, codes_left) - 1) * x_ld + x_cols : 0);
-  };
   uint32_t exps_size = uint32_t(min(int64_t(0x7fffffff), exps_more));
   const bool exps_cut = exps_more > 0x7fffffff;
-  const auto next_exps = [&] {
-    const __amdgpu_buffer_rsrc_t r = bytes_rsrc(exps_at, codes_left > 0 ? exps_size : 0);
+  __amdgpu_buffer_rsrc_t r_dy, r_codes, r_exps;
+  const auto next_dy = [&] {
+    r_dy = bytes_rsrc(dy_at, max(0, min(kSlice, dy_left) * dy_ld - (dy_ld - dy_cols)));
+    dy_at += kSlice * dy_ld;
+    dy_left -= kSlice;
+  };
+  const auto next_codes = [&] {
+    r_codes = bytes_rsrc(codes_at, max(0, min(kSlice, codes_left) * x_ld - (x_ld - x_cols)));
     codes_at += kSlice * x_ld;
+  };
+  const auto next_exps = [&] {
+    r_exps = bytes_rsrc(exps_at, codes_left > 0 ? exps_size : 0);
     exps_at += kSlice;
     codes_left -= kSlice;
     if (!exps_cut) exps_size -= kSlice;
-    return r;
+  };
+  // two slices of each, and the exponents of their 8 rows
+  BlockBf16<PN> dy[2];
+  Block<PK> x[2];
+  u32x2 xe[2];
+  const uint32_t dy_off = uint32_t(row8 * 8) * uint32_t(dy_ld) + uint32_t(col * PN * 2);
+  const uint32_t x_off = uint32_t(row8 * 8) * uint32_t(x_ld) + uint32_t(col * PK);
+  const uint32_t e_off = uint32_t(dkb) * uint32_t(q.x.le) + uint32_t(row8 * 8);
+  const auto load_dy = [&](int set, int r) {
+    const int at = int(dy_off + uint32_t(r) * uint32_t(dy_ld));
+    if constexpr (PN == 8) {
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r_dy, at, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dy[set].d[r][i] = v[i];
+    } else {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r_dy, at, 0, 0);
+      dy[set].d[r][0] = v[0];
+      dy[set].d[r][1] = v[1];
+    }
+  };
+  const auto load_codes = [&](int set, int r) {
+    const int at = int(x_off + uint32_t(r) * uint32_t(x_ld));
+    if constexpr (PK == 8) {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r_codes, at, 0, 0);
+      x[set].d[r][0] = v[0];
+      x[set].d[r][1] = v[1];
+    } else {
+      x[set].d[r][0] = __builtin_amdgcn_raw_buffer_load_b32(r_codes, at, 0, 0);
+    }
+  };
+  const auto load_exps = [&](int set) { xe[set] = __builtin_amdgcn_raw_buffer_load_b64(r_exps, int(e_off), 0, 0); };
+
+  // A slice's way to LDS in pieces of a few instructions, one or two of which go
+  // behind a product (32 cycles, which hide about seven): a column of dy; of x two
+  // columns, in four pieces: half of the rows widened, the others, each column written.
+  const auto put = [&](uint32_t at, int c, u32x4 v) {
+    *reinterpret_cast<u32x4*>(ring + at + c * (kSlice * 2) + 16 * (row8 ^ part8(c))) = v;
+  };
+  const auto put_dy = [&](int set, uint32_t stage, int c) {
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = dy[set].d[i][c / 2];
+    put(stage, col * PN + c, c % 2 ? column<true>(r) : column<false>(r));
+  };
+  float scale[8];
+  uint32_t wide[8];
+  const auto take_scale = [&](int set, int i) { scale[i] = scale8_any(xe[set][i / 4] >> (8 * (i % 4))); };
+  const auto put_x = [&](int set, uint32_t stage, int piece) {
+    const int p = piece / 4, part = piece % 4;
+    if (part < 2) {
+#pragma unroll
+      for (int i = 4 * part; i < 4 * part + 4; ++i)
+        wide[i] = p % 2 ? widened<true>(x[set].d[i][p / 2], scale[i]) : widened<false>(x[set].d[i][p / 2], scale[i]);
+    } else {
+      put(stage + kDy, col * PK + 2 * p + part - 2, part == 3 ? column<true>(wide) : column<false>(wide));
+    }
   };
 
-  // fragment addresses: a lane's granule in block f, and 8 rows further; slices
-  // of 16 rows are constants
-  const int li = lane & 15, r0 = 4 * (lane >> 5) + (li >> 2), g0 = 2 * (lane >> 4 & 1) + ((li & 3) >> 1);
+  // Fragments: columns c0 + lane % 32, rows 16 c + 8 (lane / 32) ..  of a slice.  Of
+  // block f of an operand the part differs in bit 2, of rows 16 c in bits 1 and 2.
   constexpr int NF = NB + KB, NM = NB * KB;
-  uint32_t fa[NF][2];
+  const uint32_t lds0 = lds_u32(ring);
+  uint32_t fa[2];
 #pragma unroll
-  for (int t = 0; t < NF; ++t)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int columns = t < NB ? TN : TK, c0 = t < NB ? wn * 32 * NB + t * 32 : wk * 32 * KB + (t - NB) * 32;
-      const int row = r0 + 8 * h;
-      fa[t][h] = lds0 + (t < NB ? 0 : kDy) + row * columns * 2 + 16 * ((c0 / 8 + g0) ^ swz(row)) + 8 * (li & 1);
-    }
-  i16x4 fr[2][NF][2];
-  // half h of fragment t of 16-row chunk c
-  const auto read = [&](int c, int t, int h) {
-    fr[c % 2][t][h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)uintptr_t(fa[t][h] + 16 * c * (t < NB ? TN : TK) * 2));
-  };
-  const auto frag = [&](int c, int t) {
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(fr[c % 2][t][0], fr[c % 2][t][1], 0, 1, 2, 3, 4, 5, 6, 7));
+  for (int o = 0; o < 2; ++o) {
+    const int c = (o == 0 ? wn * 32 * NB : wk * 32 * KB) + (lane & 31);
+    fa[o] = lds0 + (o == 0 ? 0 : kDy) + c * (kSlice * 2) + 16 * ((lane >> 5) ^ part8(c));
+  }
+  bf16x8 fr[2][NF];
+  const auto read = [&](int c, int t) {
+    const int o = t < NB ? 0 : 1, f = t < NB ? t : t - NB;
+    fr[c % 2][t] = *(lds_cbf16x8*)uintptr_t((fa[o] ^ uint32_t(32 * c) ^ uint32_t(64 * (f & 1))) + f * 32 * kSlice * 2);
   };
 
   f32x16 acc[NB][KB];
@@ -185,97 +211,87 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  constexpr int kNewer = (ST - 2) * (CD + NX + IX) + NX + IX;  // loads behind those of the next slice's dy
-  static_assert(kNewer <= 63, "vmcnt range");
   const int n_slices = int(s1 - s0);
-  __amdgpu_buffer_rsrc_t r_codes, r_exps;
   if (n_slices > 0) {
-    // in the order in which the loop reloads them
-    const auto load_x = [&](int set) {
-      r_codes = next_codes();
-      r_exps = next_exps();
+    // slices 0, 1 and 2 of the share, the last two of which stay in the registers
+    // (the second one's x is written: the loop takes its dy)
 #pragma unroll
-      for (int j = 0; j < NX; ++j) {
-        if (j % 4 == 0) load_exps(set, r_exps, j / 4);
-        sched_fence();
-        load_codes(set, r_codes, j);
-        sched_fence();
-      }
-    };
-    load_x(0);
+    for (int s = 0; s < 3; ++s) {
+      next_codes();
+      next_exps();
+      next_dy();
+      load_exps(s % 2);
 #pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      const __amdgpu_buffer_rsrc_t r = next_dy();
+      for (int r = 0; r < 8; ++r) load_codes(s % 2, r);
 #pragma unroll
-      for (int i = 0; i < CD; ++i) issue_dy(s * kStage, r, i);
+      for (int r = 0; r < 8; ++r) load_dy(s % 2, r);
+      if (s == 2) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) take_scale(s, i);
+#pragma unroll
+      for (int p = 0; p < 2 * PK; ++p) put_x(s, s * kStage, p);
+      if (s == 0)
+#pragma unroll
+        for (int c = 0; c < PN; ++c) put_dy(0, 0, c);
     }
-#pragma unroll
-    for (int j = 0; j < NX; ++j) {
-      xe_now = xe[0][j / 4];
-      widen(0, 0, j);
-    }
-#pragma unroll
-    for (int x = 1; x <= XD; ++x) load_x(x % XD);
-    r_codes = next_codes();
-    r_exps = next_exps();
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(XD * (NX + IX)) : "memory");
+    next_codes();
+    next_exps();
+    next_dy();
     lds_barrier();
 #pragma unroll
-    for (int t = 0; t < NF; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) read(0, t, h);
+    for (int t = 0; t < NF; ++t) read(0, t);
   }
-  uint32_t cur = 0;
-  // slice s, whose successor's codes are in `set`
+  // Slice s, in stage and register set s % 2.
   const auto slice = [&](int set) {
-    const uint32_t next = cur + kStage == ST * kStage ? 0 : cur + kStage;
-    __amdgpu_buffer_rsrc_t r_dy;
+    const uint32_t cur = set * kStage, next = kStage - cur;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      if (c == 3) {
-        // dy of the next slice has landed, its x is written
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kNewer) : "memory");
-        lds_barrier();
-      }
+      if (c == 3) lds_barrier();
 #pragma unroll
       for (int t = 0; t < NM; ++t) {
         // rows of the block are k, columns n: a lane's accumulator is of one row of dw
-        acc[t / KB][t % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(c, NB + t % KB), frag(c, t / KB),
+        acc[t / KB][t % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[c % 2][NB + t % KB], fr[c % 2][t / KB],
                                                                       acc[t / KB][t % KB], 0, 0, 0);
 #pragma unroll
-        for (int f = 0; f < 2 * NF; ++f)
-          if (f * NM / (2 * NF) == t) {
-            if (c == 3) fa[f / 2][f % 2] += next - cur;
-            read((c + 1) % 4, f / 2, f % 2);
-          }
-        if (c == 3) {
+        for (int f = 0; f < NF; ++f)
+          if (f * NM / NF == t) read((c + 1) % 4, f);
+        if (c == 0) {  // dy of slice s + 1 to LDS, x of slice s + 3 to its registers
 #pragma unroll
-          for (int i = 0; i < CD; ++i)
-            if (i * NM / CD == t) issue_dy(cur, r_dy, i);
-          if (t == NM / 2) r_codes = next_codes();
-          if (t == NM - 1) r_exps = next_exps();
-        } else {
+          for (int p = 0; p < PN; ++p)
+            if (p * NM / PN == t) put_dy(1 - set, next, p);
+          if (t == 0) load_exps(1 - set);
 #pragma unroll
-          for (int j = 0; j < NX; ++j)
-            if (j * 3 * NM / NX == c * NM + t) {
-              if (j % 4 == 0) {
-                xe_now = xe[set][j / 4];
-                load_exps(set, r_exps, j / 4);
-              }
-              widen(set, next, j);
-              load_codes(set, r_codes, j);
-            }
-          if (c == 2 && t == NM - 1) r_dy = next_dy();
+          for (int r = 0; r < 8; ++r)
+            if (r * NM / 8 == t) load_codes(1 - set, r);
+        }
+        if (c == 1) {  // dy of slice s + 3
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (r * NM / 8 == t) load_dy(1 - set, r);
+        }
+        if (c == 2) {
+          if (t == 0) next_codes();
+          if (t == NM / 4) next_exps();
+          if (t == NM / 2) next_dy();
+          if (t == NM - 1) fa[0] += next - cur, fa[1] += next - cur;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i * NM / 8 == t) take_scale(set, i);
+        }
+        if (c == 3) {  // x of slice s + 2, into the stage that has been read
+#pragma unroll
+          for (int p = 0; p < 2 * PK; ++p)
+            if (p * NM / (2 * PK) == t) put_x(set, cur, p);
         }
         sched_fence();
       }
     }
-    cur = next;
   };
-  for (int s = 0; s < n_slices; s += XD)
-#pragma unroll
-    for (int x = 1; x <= XD; ++x) slice(x % XD);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the work-group
+  for (int s = 0; s + 1 < n_slices; s += 2) {
+    slice(0);
+    slice(1);
+  }
+  if (n_slices & 1) slice(0);
 
   if (share >= 0 && q.splits > 1) {
     f32x4* out = reinterpret_cast<f32x4*>(q.partial) + share * (TN * TK / 4) + tid;
@@ -285,7 +301,7 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
       for (int j = 0; j < KB; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          out[((i * KB + j) * 4 + r) * (NW * 64)] =
+          out[((i * KB + j) * 4 + r) * 256] =
               f32x4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
   } else {
 #pragma unroll
@@ -304,38 +320,40 @@ __global__ __launch_bounds__(WN * WK * 64) __attribute__((amdgpu_waves_per_eu(1,
   }
 }
 
-// A work-group adds, in the order of the shares, one row of a tile's accumulator
-// blocks (the same 32 x 32 block of every wave).
+// A work-group adds, in the order of the shares, a quarter of a tile's accumulator
+// blocks (i, j) of every wave, four shares' loads in flight.
 template <int NB, int KB, int WN, int WK>
-__global__ __launch_bounds__(WN * WK * 64) void wgrad8_join_kernel(const WGrad8Params q) {
-  constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK, kBlocks = NB * KB;
+__global__ __launch_bounds__(256) void wgrad8_join_kernel(const WGrad8Params q) {
+  constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK, kParts = NB * KB * 4, kAhead = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wn = wave / WK, wk = wave % WK;
-  const int64_t rows_n = (q.N + TN - 1) / TN, cols_k = (q.K + TK - 1) / TK, tiles = rows_n * cols_k;
-  const int64_t rest = tiles - q.whole, t = int64_t(blockIdx.x) / kBlocks;
-  const int block = int(blockIdx.x % kBlocks), i = block / KB, j = block % KB;
-  f32x4 v[4] = {};
-  for (int s = 0; s < q.splits; ++s) {
-    const f32x4* in = reinterpret_cast<const f32x4*>(q.partial) + (s * rest + t) * (TN * TK / 4) + tid;
+  const int64_t rows_n = (q.N + TN - 1) / TN, cols_k = (q.K + TK - 1) / TK;
+  const int64_t rest = rows_n * cols_k - q.whole, t = int64_t(blockIdx.x) / kParts;
+  const int part = int(blockIdx.x % kParts), i = part / 4 / KB, j = part / 4 % KB;
+  const f32x4* in = reinterpret_cast<const f32x4*>(q.partial) + t * (TN * TK / 4) + part * 256 + tid;
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < q.splits; s += kAhead) {
+    f32x4 w[kAhead];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] += in[(block * 4 + r) * (WN * WK * 64)];
+    for (int u = 0; u < kAhead; ++u) w[u] = in[min(s + u, q.splits - 1) * rest * (TN * TK / 4)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s + u < q.splits) v += w[u];
   }
   int64_t tn, tk;
   grouped_tile(q.whole + t, rows_n, cols_k, 4, tn, tk);
   const int64_t n = tn * TN + wn * 32 * NB + i * 32 + (lane & 31);
-  const int64_t k = tk * TK + wk * 32 * KB + j * 32 + 4 * (lane >> 5);
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (n < q.N && k + 8 * r < q.K) *reinterpret_cast<f32x4*>(q.dw + n * q.lddw + k + 8 * r) = v[r];
+  const int64_t k = tk * TK + wk * 32 * KB + j * 32 + 4 * (lane >> 5) + part % 4 * 8;
+  if (n < q.N && k < q.K) *reinterpret_cast<f32x4*>(q.dw + n * q.lddw + k) = v;
 }
 
-template <int NB, int KB, int WN, int WK, int ST, int XD>
+template <int NB, int KB, int WN, int WK>
 void launch_tile(const WGrad8Params& q, hipStream_t s) {
   constexpr int TN = 32 * NB * WN, TK = 32 * KB * WK;
   const int64_t rest = int64_t((q.N + TN - 1) / TN) * ((q.K + TK - 1) / TK) - q.whole;
-  hipLaunchKernelGGL((wgrad8_kernel<NB, KB, WN, WK, ST, XD>), dim3(q.whole + rest * q.splits), dim3(WN * WK * 64), 0, s, q);
+  hipLaunchKernelGGL((wgrad8_kernel<NB, KB, WN, WK>), dim3(q.whole + rest * q.splits), dim3(WN * WK * 64), 0, s, q);
   if (q.splits > 1)
-    hipLaunchKernelGGL((wgrad8_join_kernel<NB, KB, WN, WK>), dim3(rest * NB * KB), dim3(WN * WK * 64), 0, s, q);
+    hipLaunchKernelGGL((wgrad8_join_kernel<NB, KB, WN, WK>), dim3(rest * NB * KB * 4), dim3(256), 0, s, q);
 }
 
 }  // namespace
@@ -343,9 +361,9 @@ void launch_tile(const WGrad8Params& q, hipStream_t s) {
 int launch_wgrad8(const WGrad8Params& q, int32_t tile, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   switch (tile) {
-    case 0: launch_tile<4, 4, 2, 2, 2, 1>(q, s); break;
-    case 1: launch_tile<4, 2, 2, 2, 3, 2>(q, s); break;
-    default: launch_tile<2, 2, 2, 2, 4, 2>(q, s); break;
+    case 0: launch_tile<4, 4, 2, 2>(q, s); break;
+    case 1: launch_tile<4, 2, 2, 2>(q, s); break;
+    default: launch_tile<2, 2, 2, 2>(q, s); break;
   }
   return int(hipGetLastError());
 }
