@@ -618,6 +618,8 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
         _blocks(out, "out", M, K)
         if transposed:
             _blocks(out.t, "out.t", K, M)
+        elif out.t is not None:
+            raise ValueError("out has a transposed form, which would stay what it is: transposed=True, or another out")
         _same_device(dev, out=out)
     _call(lib().rc_quantize_blocks, dev, stream, M, K, x.data_ptr(), ldx, int(square), ctypes.byref(out.c),
           ctypes.byref(out.t.c) if transposed else None)

@@ -1465,10 +1465,16 @@ rc_status check_workspace8(const char* what, const void* workspace, size_t have,
   return RC_OK;
 }
 
-// Work-groups of the largest launch over [M, N] outputs and [M, K] rows.
-rc_status check_grid8(int64_t M, int64_t N, int64_t K, const char* what) {
-  RC_TRY(check_blocks((M + 63) / 64 * ((N + 63) / 64), what));
-  return check_blocks((M + 31) / 32 * ((blocks8(K) + 3) / 4), what);
+// The launches of a product of [M, K] rows (bf16: quantised on the way) with [N, K].
+rc_status check_product8(int64_t M, int32_t N, int32_t K, bool bf16, const char* what) {
+  if (bf16 && few_rows8(M, N, K)) return check_threads((M + 15) / 16 * ((N + 15) / 16), 512, what);
+  const Tile8 t = kLinear8Tiles[plan_linear8(M, N, K)];
+  RC_TRY(check_threads((M + t.bm - 1) / t.bm * ((N + t.bn - 1) / t.bn), 512, what));
+  return bf16 ? check_threads((M + 31) / 32 * ((blocks8(K) + 3) / 4), 256, what) : RC_OK;
+}
+
+rc_status check_wgrad8(int64_t M, int32_t N, int32_t K, const char* what) {
+  return check_threads(plan_wgrad8(M, N, K).blocks(), 256, what);
 }
 
 rc_status run_linear8(int64_t M, int32_t N, int32_t K, Linear8Params& q, const void* r, int64_t ldr, void* out,
@@ -1525,7 +1531,8 @@ rc_status rc_quantize_blocks(int64_t M, int32_t K, const void* x, int64_t ldx, i
     RC_TRY(check_size8("block quantisation, transposed", K, M, 8));
     RC_TRY(check_blocks8(out_t, K, M, "out_t"));
   }
-  RC_TRY(check_grid8(M, 8, K, "block quantisation"));
+  RC_TRY(check_threads(square ? blocks8(M) * blocks8(K) : (M + 31) / 32 * ((blocks8(K) + 3) / 4), 256,
+                       "block quantisation"));
   RC_TRY(check_launcher(launch_quantize_rows, "block quantisation"));
   const Quant8Params q{static_cast<const uint16_t*>(x), ldx, M, K, blocks_of(out),
                        out_t ? blocks_of(out_t) : Blocks8{nullptr, 0, nullptr, 0}};
@@ -1539,7 +1546,7 @@ rc_status rc_dequantize_blocks(int64_t M, int32_t K, const rc_blocks8* x, void* 
   RC_TRY(check_blocks8(x, M, K, "x"));
   RC_TRY(check_ptr(out, "out"));
   RC_TRY(check_ld8(ldo, K, "out"));
-  RC_TRY(check_blocks((M * (K / 8) + 255) / 256, "block expansion"));
+  RC_TRY(check_threads((M * (K / 8) + 255) / 256, 256, "block expansion"));
   RC_TRY(check_launcher(launch_dequantize, "block expansion"));
   const Dequant8Params q{blocks_of(x), M, K, static_cast<uint16_t*>(out), ldo};
   return hip_status(launch_dequantize(q, stream), "block expansion launch");
@@ -1553,7 +1560,7 @@ rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8
   RC_TRY(check_blocks8(a, M, K, "a"));
   RC_TRY(check_blocks8(w, N, K, "w"));
   RC_TRY(check_out8(N, r, ldr, out, ldo));
-  RC_TRY(check_grid8(M, N, K, "FP8 linear"));
+  RC_TRY(check_product8(M, N, K, false, "FP8 linear"));
   RC_TRY(check_launcher(launch_linear8, "FP8 linear"));
   Linear8Params q{};
   q.a = blocks_of(a);
@@ -1563,7 +1570,8 @@ rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8
 
 size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K) {
   using namespace rc;
-  return check_size8("FP8 linear", M, N, K) == RC_OK ? linear8_workspace(M, N, K) : 0;
+  const bool ok = check_size8("FP8 linear", M, N, K) == RC_OK && check_product8(M, N, K, true, "FP8 linear") == RC_OK;
+  return ok ? linear8_workspace(M, N, K) : 0;
 }
 
 rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t lda, const rc_blocks8* w,
@@ -1576,7 +1584,7 @@ rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t 
   RC_TRY(check_ld8(lda, K, "a"));
   RC_TRY(check_blocks8(w, N, K, "w"));
   RC_TRY(check_out8(N, r, ldr, out, ldo));
-  RC_TRY(check_grid8(M, N, K, "FP8 linear"));
+  RC_TRY(check_product8(M, N, K, true, "FP8 linear"));
   RC_TRY(check_workspace8("FP8 linear", workspace, ws_bytes, linear8_workspace(M, N, K)));
   RC_TRY(check_launcher(launch_linear8, "FP8 linear"));
   Linear8Params q{};
@@ -1588,7 +1596,10 @@ rc_status rc_linear_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t 
 
 size_t rc_linear_fp8_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t want_dx, int32_t want_dw) {
   using namespace rc;
-  if (check_size8("FP8 linear's gradient", M, N, K) != RC_OK) return 0;
+  const char* what = "FP8 linear's gradient";
+  if (check_size8(what, M, N, K) != RC_OK) return 0;
+  if (want_dx && check_product8(M, K, N, true, what) != RC_OK) return 0;
+  if (want_dw && check_wgrad8(M, N, K, what) != RC_OK) return 0;
   return (want_dx ? round16(linear8_workspace(M, K, N)) : 0) + (want_dw ? plan_wgrad8(M, N, K).partial_bytes() : 0);
 }
 
@@ -1613,14 +1624,13 @@ rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy
   if (dx && M > 0) {
     RC_TRY(check_blocks8(w_t, K, N, "w_t"));
     RC_TRY(check_out8(K, r, ldr, dx, lddx));
-    RC_TRY(check_grid8(M, K, N, "FP8 linear's gradient"));
+    RC_TRY(check_product8(M, K, N, true, "FP8 linear's gradient"));
   }
   if (dw) {
     RC_TRY(check_ptr(dw, "dw"));
     RC_TRY(check_ld8(lddw, K, "dw"));
     if (M > 0) RC_TRY(check_blocks8(x, M, K, "x"));
-    const WGrad8Plan plan = plan_wgrad8(M, N, K);
-    RC_TRY(check_blocks(plan.blocks(), "FP8 weights' gradient"));
+    RC_TRY(check_wgrad8(M, N, K, "FP8 weights' gradient"));
   }
   RC_TRY(check_workspace8("FP8 linear's gradient", workspace, ws_bytes,
                           rc_linear_fp8_backward_workspace_bytes(M, N, K, dx != nullptr, dw != nullptr)));

@@ -80,7 +80,7 @@ int launch_wgrad8(const WGrad8Params& q, int32_t tile, void* stream) RC_WEAK;
 // group of 32 rows (80 x 384 x 128 3.6 us, as much as the quantisation alone).
 constexpr int64_t kFewRows8 = 32, kFewRead8 = int64_t(4) << 20;
 constexpr bool few_rows8(int64_t M, int32_t N, int32_t K) {
-  return M <= kFewRows8 || (M + 31) / 32 * N * pad8(K) <= kFewRead8;
+  return M <= kFewRows8 || (M + 31) / 32 <= kFewRead8 / (N * pad8(K));
 }
 
 struct Tile8 {

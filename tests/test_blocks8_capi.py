@@ -134,8 +134,15 @@ def test_no_rows_and_launch_limits():
     assert dequant(M=0, x=None, out=None) == rc.RC_OK
     assert linear(M=0, a=None, out=None, ws=None, wsb=0) == linear_blocks(M=0, a=None, out=None) == rc.RC_OK
     assert back(M=0, dx=None, dw=None, dy=None, x=None, w_t=None, ws=None, wsb=0) == rc.RC_OK
-    big = dict(M=1 << 28, N=1 << 22, K=128, lda=128, ldo=1 << 22)
-    assert linear(**big) == rc.RC_ERR_ARG and "grid" in message()
+    # a launch has fewer than 2^32 threads: refused by the call, and 0 from the queries
+    big = dict(M=1 << 28, N=1 << 22, K=128)
+    assert linear(lda=128, ldo=1 << 22, **big) == rc.RC_ERR_ARG and "launch" in message()
+    assert linear_blocks(ldo=1 << 22, **big) == rc.RC_ERR_ARG and "launch" in message()
+    assert rc.lib().rc_linear_fp8_workspace_bytes(*big.values()) == 0
+    assert back(lddy=1 << 22, lddx=128, lddw=128, **big) == rc.RC_ERR_ARG and "launch" in message()
+    assert quant(M=1 << 28, K=1 << 22, ldx=1 << 22, square=0, out_t=None) == rc.RC_ERR_ARG and "launch" in message()
+    assert dequant(M=1 << 28, K=1 << 20, ldo=1 << 20) == rc.RC_ERR_ARG and "launch" in message()
+    assert rc.lib().rc_linear_fp8_backward_workspace_bytes(1 << 28, 1 << 22, 128, 1, 0) == 0
 
 
 # ---------------------------------------------------------------- the binding
