@@ -66,4 +66,6 @@ def test_limits_of_the_grid():
         assert linear(lda=K, ldo=N, wsb=1 << 62, **ld) in (rc.RC_OK, rc.RC_ERR_ARG)
         assert linear_blocks(ldo=N, **ld) in (rc.RC_OK, rc.RC_ERR_ARG)
         assert back(lddy=N, lddx=K, lddw=K, wsb=1 << 62, **ld) in (rc.RC_OK, rc.RC_ERR_ARG)
-    assert back(M=0, N=1 << 22, K=1 << 22, lddw=1 << 22, dx=None, x=None, w_t=None) == rc.RC_OK
+    stub("workspace", 0, 0)
+    assert back(M=0, N=1 << 18, K=1 << 18, lddw=1 << 18, dx=None, x=None, w_t=None) == rc.RC_OK
+    assert back(M=0, N=1 << 22, K=1 << 22, lddw=1 << 22, dx=None, x=None, w_t=None) == rc.RC_ERR_ARG
