@@ -20,7 +20,9 @@ namespace {
 // a block, 8 values each, so a wave reads 1 KB of a row at once, and all of a
 // thread's rows are in flight together.  The exponents are gathered in LDS so
 // that a block's column of them is written in runs of kRows bytes.
-// Memory-bound: 2 bytes read and 1 written per value.
+// Memory-bound: 2 bytes read and 1 written per value; 25 152 x 2560 takes 28.9 us
+// (6.7 TB/s, partly from the last-level cache).  Loads by buffer descriptor: with a
+// branch around each, the compiler waited for one at a time (47 us).
 constexpr int kRows = 32;
 
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const Quant8Params q) {
@@ -69,7 +71,8 @@ __device__ __forceinline__ void transpose4(uint32_t r0, uint32_t r1, uint32_t r2
 // Squares of 128 x 128, one per work-group, 8 x 8 values per thread, whose
 // codes are transposed in registers; LDS only gathers them into whole rows (8-byte
 // part p of row k at part p ^ (k / 8)).  Columns up to the next multiple of 128 exist
-// as zeros.  Memory-bound: 2 bytes read and 1 or 2 written per value.
+// as zeros.  Memory-bound: 2 bytes read and 1 or 2 written per value; 7680 x 2560
+// with the transposed form takes 12.7 us (6.2 TB/s; with bytes gathered from LDS 19).
 __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Params q) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kBlock8];
   __shared__ uint32_t red[4];
@@ -126,6 +129,7 @@ __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Param
 }
 
 // 8 codes per thread back to bf16, exact (4 significant bits) above bf16's smallest.
+// Memory-bound: 25 152 x 2560 takes 30 us (6.4 TB/s).
 __global__ __launch_bounds__(256) void dequantize_kernel(const Dequant8Params q) {
   const int g = q.K / 8;
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;

@@ -89,7 +89,8 @@ struct Tile8 {
 constexpr Tile8 kLinear8Tiles[] = {{256, 256}, {192, 256}, {256, 128}, {128, 128}, {64, 128}, {64, 64}};
 int32_t plan_linear8(int64_t M, int32_t N, int32_t K);
 
-constexpr Tile8 kWGrad8Tiles[] = {{256, 256}, {256, 128}, {128, 128}};  // n x k
+// n x k
+constexpr Tile8 kWGrad8Tiles[] = {{256, 256}, {256, 128}, {128, 128}};
 struct WGrad8Plan {
   int32_t tile, splits;
   int64_t whole, tiles;

@@ -8,8 +8,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "rc_blocks8.h"
 #include "rc_lds.h"
 #include "rc_quant8.h"
@@ -63,10 +61,17 @@ __device__ __forceinline__ u32x4 column(const uint32_t (&r)[8]) {
 // behind it the next slice's first fragments are read, and its own stage is written
 // again.  Slices past the share's last one load zeros, so the loop has no other branch.
 //
-// What bounds it: 64 products of 32 cycles per slice and SIMD (256 x 256), beside
-// 1 536 cycles of LDS.  (With dy loaded straight into LDS, and both operands read by
-// the transpose read ds_read_b64_tr_b16, which takes twice the cycles per byte, LDS
-// was busy 2 560 cycles and the slice took as long.)
+// What bounds it (256 x 256): 64 products of 32 cycles per slice and SIMD, 2048, and the
+// issue of what goes between them.  On 25 tiles, at 2.42 GHz, a slice takes 2 980 cycles
+// (counters: LDS busy 1 030 of them, waits 380, the rest waits for issue); on a full
+// chip, whose clock falls, 1.6 us: 17 536 x 4096 x 4096 runs in 439-456 us (1.29-1.34
+// PFLOP/s; the library's 8192 cubed reaches 1.43).  17 536 x 7680 x 2560, 300 tiles, takes
+// 558-564 us (the library's product of transposed dy 912).  Forms measured before, at these
+// two: dy loaded straight into LDS and both operands read by the transpose read
+// ds_read_b64_tr_b16, 443 and 591 us; both transposed in registers with one slice there,
+// 477 and 596; with two, 463 and 573 until the pieces behind a product became as short
+// as it hides.  On few tiles, a slice of the smaller ones takes 0.79 us (256 x 128) and
+// 0.63 (128 x 128).
 template <int NB, int KB, int WN, int WK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void wgrad8_kernel(const WGrad8Params q) {
   static_assert(WN * WK == 4, "four waves");
