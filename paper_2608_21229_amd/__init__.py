@@ -3,7 +3,8 @@ path of arXiv 2608.21229: block-masked attention over
 [static text anchors | live text | target | references], with a
 once-per-request reference K/V prefill, per-step masked attention over fresh
 plus cached K/V, and a full-recompute baseline; for training, the gradient of
-the recompute, and the norms and rotation around the attention with theirs.
+the recompute, and the norms and rotation around the attention with theirs;
+and projections in 8 bits with a scale per block of 128 values.
 
 The compute lives in ``librefcache.so`` (hand-written HIP, C ABI declared in
 ``include/refcache.h``); ``binding`` is its ctypes wrapper and ``chain``
