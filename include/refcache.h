@@ -483,6 +483,7 @@ size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);  /* 0 on invali
  * exact); infinities and NaN become NaN.
  * Sizes: 0 <= rows <= 2^28, columns multiples of 8 from 8 to 2^22.  Pointers 16-byte aligned; row strides of
  * bf16 and fp32 matrices in elements, multiples of 8, <= 2^22.  Outputs overlap no input except as said.
+ * A workspace serves one call at a time: calls and graph replays that may overlap need one each.
  * RC_ERR_UNSUPPORTED for columns off those multiples, RC_ERR_ARG otherwise.  rows = 0 is a no-op. */
 typedef struct {
   void* codes;

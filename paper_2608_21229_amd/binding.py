@@ -639,15 +639,18 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     """out = a @ w.T (+ residual) in 8 bits: w [N, K] Fp8Blocks, a [M, K] Fp8Blocks
     or bf16 (any row stride; quantised per 128 values of a row on the way, into the
     workspace); bf16 out, fp32 accumulation.  residual, out: [M, N] (any row
-    stride; out may be residual).  A row's result does not depend on M for
+    stride; out may be residual, not a).  A row's result does not depend on M for
     Fp8Blocks; a small bf16 call (up to 32 rows, or little work) sums in another order.
     Returns out."""
     L, blocks = lib(), isinstance(a, Fp8Blocks)
     lda = 0 if blocks else _rows_view(a, "a")
     M, K = _blocks(a, "a") if blocks else a.shape
     dev, N = a.device, _blocks(w, "w", cols=K)[0]
+    given = out is not None
     out, ldo = _rows_out(out, "out", M, N, dev, stream)
     ldr = _rows_in(residual, "residual", M, N, dev)
+    if given:
+        _apart(out, "out", ldo, None if blocks else a, "a", residual, ldr)
     if w.device != dev:
         raise ValueError(f"w is on {w.device}, the inputs on {dev}")
     if blocks:
@@ -668,6 +671,17 @@ def _rows_out(t, what, rows, cols, dev, stream):
     return t, _rows_in(t, what, rows, cols, dev)
 
 
+def _apart(out, what, ldo, a, name, residual, ldr):
+    """Refuses the caller's output where it is the input a, or the residual at another row stride."""
+    at = out.data_ptr()
+    if out.numel() == 0:
+        return
+    if a is not None and a.data_ptr() == at:
+        raise ValueError(f"{what} may not be {name}, which is read while it is written")
+    if residual is not None and ldr != ldo and residual.data_ptr() == at:
+        raise ValueError(f"{what} may be residual only with its row stride, {ldr}, got {ldo}")
+
+
 def _rows_in(t, what, rows, cols, dev):
     """The row stride of a checked bf16 [rows, cols] tensor; 0 for None."""
     if t is None:
@@ -685,8 +699,8 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     """The gradient of linear_fp8 for dy [M, N] bf16: x [M, K] Fp8Blocks, the input
     that the product has read; w [N, K] Fp8Blocks with their transposed form.
     dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row;
-    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual.  Returns (dx, dw), None
-    for what is not wanted (x and w may then be None)."""
+    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual, not dy.  A workspace serves one
+    call at a time.  Returns (dx, dw), None for what is not wanted (x and w may then be None)."""
     L, lddy, lddx, ldr, w_t = lib(), _rows_view(dy, "dy"), 0, 0, None
     dev = dy.device
     M, N = dy.shape
@@ -702,8 +716,11 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
         if w_t is None:
             raise ValueError("w has no transposed form: quantize_blocks(w, square=True, transposed=True)")
         _blocks(w_t, "w.t", K, N)
+        given = dx is not None
         dx, lddx = _rows_out(dx, "dx", M, K, dev, stream)
         ldr = _rows_in(residual, "residual", M, K, dev)
+        if given:
+            _apart(dx, "dx", lddx, dy, "dy", residual, ldr)
     if want_dw:
         _blocks(x, "x", M, K)
         if dw is None:
@@ -724,6 +741,8 @@ def _workspace(workspace, need, dev, stream):
     if workspace is None or workspace.numel() * workspace.element_size() < need:
         return _empty(need, _torch().uint8, dev, stream, returned=False)
     _same_device(dev, workspace=workspace)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     return workspace
 
 

@@ -171,3 +171,28 @@ def test_blocks_shapes():
     with pytest.raises(ValueError, match="t must be"):
         cpu_blocks(8, 136, cpu_blocks(8, 136))
     assert cpu_blocks(8, 136, cpu_blocks(136, 8)).t.shape == (136, 8)
+
+
+def test_strided_workspaces_are_refused():
+    """A workspace is written as one run of bytes: a view of every second has half of them."""
+    dev, whole = torch.device("cpu"), torch.zeros(128, dtype=torch.uint8)
+    assert binding._workspace(whole, 64, dev, None) is whole
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._workspace(whole[::2], 64, dev, None)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._workspace(torch.zeros(16, 8, dtype=torch.float32)[:, :4], 64, dev, None)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._workspace(torch.zeros(1, dtype=torch.uint8).expand(64), 64, dev, None)
+
+
+def test_outputs_over_inputs_are_refused():
+    """Tiles are written while others still read: an output may be the residual as it lies, and nothing else."""
+    m = torch.zeros(8, 512, dtype=torch.bfloat16)
+    x, other = m[:, :128], m[:, 128:256]
+    binding._apart(x, "out", 512, other, "a", x, 512)
+    binding._apart(x, "out", 512, other, "a", None, 0)
+    binding._apart(m[:0], "out", 512, m[:0], "a", None, 0)
+    with pytest.raises(ValueError, match="out may not be a"):
+        binding._apart(x, "out", 512, x, "a", None, 0)
+    with pytest.raises(ValueError, match="stride"):
+        binding._apart(x, "out", 512, other, "a", m.view(32, 128)[:8], 128)
