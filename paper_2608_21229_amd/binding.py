@@ -621,6 +621,9 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
         elif out.t is not None:
             raise ValueError("out has a transposed form, which would stay what it is: transposed=True, or another out")
         _same_device(dev, out=out)
+        _apart_from(out, "out", x=x)
+        if transposed:
+            _apart_from(out.t, "out.t", x=x, out=out)
     _call(lib().rc_quantize_blocks, dev, stream, M, K, x.data_ptr(), ldx, int(square), ctypes.byref(out.c),
           ctypes.byref(out.t.c) if transposed else None)
     return out
@@ -629,8 +632,10 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
 def dequantize_blocks(x, out=None, stream=None):
     """The values of Fp8Blocks in bf16 [M, K] (exact).  Returns out."""
     M, K = _blocks(x, "x")
-    dev = x.device
+    dev, given = x.device, out is not None
     out, ldo = _rows_out(out, "out", M, K, dev, stream)
+    if given:
+        _apart_from(out, "out", x=x)
     _call(lib().rc_dequantize_blocks, dev, stream, M, K, ctypes.byref(x.c), out.data_ptr(), ldo)
     return out
 
@@ -639,7 +644,8 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     """out = a @ w.T (+ residual) in 8 bits: w [N, K] Fp8Blocks, a [M, K] Fp8Blocks
     or bf16 (any row stride; quantised per 128 values of a row on the way, into the
     workspace); bf16 out, fp32 accumulation.  residual, out: [M, N] (any row
-    stride; out may be residual, not a).  A row's result does not depend on M for
+    stride; out may be residual as it lies).  What is given to write to (out, workspace) may lie
+    beside the inputs in one buffer, but shares no memory with them.  A row's result does not depend on M for
     Fp8Blocks; a small bf16 call (up to 32 rows, or little work) sums in another order.
     Returns out."""
     L, blocks = lib(), isinstance(a, Fp8Blocks)
@@ -651,6 +657,7 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     ldr = _rows_in(residual, "residual", M, N, dev)
     if given:
         _apart(out, "out", ldo, None if blocks else a, "a", residual, ldr)
+        _apart_from(out, "out", a=a if blocks else None, w=w)
     if w.device != dev:
         raise ValueError(f"w is on {w.device}, the inputs on {dev}")
     if blocks:
@@ -658,7 +665,9 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
               out.data_ptr(), ldo)
         return out
     need = L.rc_linear_fp8_workspace_bytes(M, N, K)
-    workspace = _workspace(workspace, need, dev, stream) if need else None
+    workspace, own = (_workspace(workspace, need, dev, stream) if need else None), workspace
+    if need and workspace is own:
+        _apart_from(((own.data_ptr(), need, need, 1),), "workspace", a=a, w=w, residual=residual, out=out)
     _call(L.rc_linear_fp8, dev, stream, M, N, K, a.data_ptr(), lda, ctypes.byref(w.c), _ptr(residual), ldr,
           out.data_ptr(), ldo, _ptr(workspace), need)
     return out
@@ -672,14 +681,57 @@ def _rows_out(t, what, rows, cols, dev, stream):
 
 
 def _apart(out, what, ldo, a, name, residual, ldr):
-    """Refuses the caller's output where it is the input a, or the residual at another row stride."""
+    """Refuses the caller's output where it shares memory with the input a (None: no bf16 one), or with the
+    residual other than as it lies."""
     at = out.data_ptr()
     if out.numel() == 0:
         return
-    if a is not None and a.data_ptr() == at:
-        raise ValueError(f"{what} may not be {name}, which is read while it is written")
-    if residual is not None and ldr != ldo and residual.data_ptr() == at:
+    if a is not None and _meet(_rows_at(out), _rows_at(a)):
+        raise ValueError(f"{what} may not be {name}, which is read while it is written, nor overlap it")
+    if residual is None or (ldr == ldo and residual.data_ptr() == at):
+        return
+    if residual.data_ptr() == at:
         raise ValueError(f"{what} may be residual only with its row stride, {ldr}, got {ldo}")
+    if _meet(_rows_at(out), _rows_at(residual)):
+        raise ValueError(f"{what} may be residual as it lies, but not overlap it otherwise")
+
+
+def _apart_from(t, what, **others):
+    """Refuses a caller's output (a tensor or Fp8Blocks) or a workspace's place that shares memory with
+    others, None where absent, which the call reads or writes too."""
+    mine = t if isinstance(t, tuple) else _places(t)
+    for name, o in others.items():
+        if o is not None and any(_meet(a, b) for b in _places(o) for a in mine):
+            raise ValueError(f"{what} may not overlap {name}")
+
+
+def _rows_at(t):
+    """Where a tensor lies: (address, bytes of a row, bytes from one row to the next, rows).  One that
+    is no matrix is contiguous here: one row."""
+    size = t.element_size()
+    if t.dim() == 2 and not t.is_contiguous():
+        return t.data_ptr(), t.shape[1] * size, t.stride(0) * size, t.shape[0]
+    n = t.numel() * size
+    return t.data_ptr(), n, n, 1
+
+
+def _places(t):
+    """The same of all that a tensor or Fp8Blocks (without their transposed form) hold."""
+    if not isinstance(t, Fp8Blocks):
+        return (_rows_at(t),)
+    codes, exps = t.shape[0] * t.c.ld, -(-t.shape[1] // 128) * t.c.ld_exps
+    return (t.c.codes or 0, codes, codes, 1), (t.c.exps or 0, exps, exps, 1)
+
+
+def _meet(a, b):
+    """Whether two places of _rows_at share a byte: their ranges do, and they are not columns side by
+    side, which stay apart in every row where they do in one (modulo what divides both strides)."""
+    (p, w, s, n), (q, v, u, m) = a, b
+    if not (n and m and w and v) or p + (n - 1) * s + w <= q or q + (m - 1) * u + v <= p:
+        return False
+    g = math.gcd(s if n > 1 else 0, u if m > 1 else 0)
+    r = (q - p) % g if g else 0
+    return not (w <= r <= g - v)
 
 
 def _rows_in(t, what, rows, cols, dev):
@@ -699,7 +751,8 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     """The gradient of linear_fp8 for dy [M, N] bf16: x [M, K] Fp8Blocks, the input
     that the product has read; w [N, K] Fp8Blocks with their transposed form.
     dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row;
-    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual, not dy.  A workspace serves one
+    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual as it lies; otherwise dx,
+    dw and workspace share no memory with the inputs or each other.  A workspace serves one
     call at a time.  Returns (dx, dw), None for what is not wanted (x and w may then be None)."""
     L, lddy, lddx, ldr, w_t = lib(), _rows_view(dy, "dy"), 0, 0, None
     dev = dy.device
@@ -711,6 +764,8 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     if (dx is not None and not want_dx) or (dw is not None and not want_dw):
         raise ValueError("dx or dw is given but not wanted")
     K = (_blocks(w, "w", rows=N) if want_dx else _blocks(x, "x", rows=M))[1]
+    if want_dw:
+        _blocks(x, "x", M, K)
     if want_dx:
         w_t = w.t
         if w_t is None:
@@ -721,16 +776,20 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
         ldr = _rows_in(residual, "residual", M, K, dev)
         if given:
             _apart(dx, "dx", lddx, dy, "dy", residual, ldr)
+            _apart_from(dx, "dx", w=w_t, x=x if want_dw else None)
     if want_dw:
-        _blocks(x, "x", M, K)
         if dw is None:
             dw = _empty((N, K), _torch().float32, dev, stream)
         else:
             _expect(dw, (N, K), "torch.float32", "dw")
             _same_device(dev, dw=dw)
+            _apart_from(dw, "dw", dy=dy, x=x, w=w_t, residual=residual, dx=dx)
     _same_device(dev, x=x if want_dw else None, w=w_t)
     need = L.rc_linear_fp8_backward_workspace_bytes(M, N, K, int(want_dx), int(want_dw))
-    workspace = _workspace(workspace, need, dev, stream) if need else None
+    workspace, own = (_workspace(workspace, need, dev, stream) if need else None), workspace
+    if need and workspace is own:
+        _apart_from(((own.data_ptr(), need, need, 1),), "workspace", dy=dy, x=x if want_dw else None, w=w_t,
+                    residual=residual, dx=dx, dw=dw)
     _call(L.rc_linear_fp8_backward, dev, stream, M, N, K, dy.data_ptr(), lddy, ctypes.byref(x.c) if want_dw else None,
           ctypes.byref(w_t.c) if want_dx else None, _ptr(residual), ldr, _ptr(dx), lddx, _ptr(dw), K, _ptr(workspace), need)
     return dx, dw
