@@ -500,9 +500,13 @@ rc_status rc_quantize_blocks(int64_t M, int32_t K, const void* x, int64_t ldx, i
 /* The values in bf16 (exact from 2^-133 on). */
 rc_status rc_dequantize_blocks(int64_t M, int32_t K, const rc_blocks8* x, void* out, int64_t ldo, void* stream);
 
-/* out[m, n] = bf16( sum_k a[m, k] w[n, k] (+ r[m, n]) ) of the values of a [M, K] and w [N, K], fp32
- * accumulation in a fixed order, one RNE rounding.  A row's result depends on its own values only and is
- * the same for every M.  r nullable; out may be r (same stride). */
+/* out[m, n] = bf16( sum_k a[m, k] w[n, k] (+ r[m, n]) ) of the values of a [M, K] and w [N, K], summed in fp32
+ * in a fixed order, one RNE rounding.  The products are cut before they are summed: of eight neighbours (of
+ * one k / 8) each is cut towards zero to a multiple of 2^-13 2^p, where 2^p is the largest product among them of
+ * the powers of two in both codes (2^-6 for codes below 2^-6; zero products count nothing) and of both scales.
+ * With codes from 2^-6 on a product so loses less than 2^-13 of the largest of its eight, and nothing where that
+ * is at most 2^7 times itself (powers of two); with smaller codes less than 2^-10.  A row's result depends on its
+ * own values only and is the same for every M.  r nullable; out may be r (same stride). */
 rc_status rc_linear_fp8_blocks(int64_t M, int32_t N, int32_t K, const rc_blocks8* a, const rc_blocks8* w,
                                const void* r, int64_t ldr, void* out, int64_t ldo, void* stream);
 
@@ -516,7 +520,8 @@ size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K);  /* 0 on 
 
 /* The gradient of rc_linear_fp8_blocks for dy [M, N] bf16.
  *   dx [M, K] bf16  = sum_n dy[m, n] w[n, k] (+ r[m, k]): rc_linear_fp8 of dy, quantised in blocks of a row,
- *                     and w_t, the transposed weights [K, N]; NULL: not wanted, w_t and r are then NULL
+ *                     and w_t, the transposed weights [K, N] (products cut as there); NULL: not wanted, w_t and r
+ *                     are then NULL
  *   dw [N, K] fp32  = sum_m dy[m, n] x[m, k], of dy as it is and of the values of x [M, K], the product's input,
  *                     which is its own checkpoint; zeros for M = 0; NULL: not wanted, x is then NULL
  * r may be dx (same stride).  Workspace: rc_linear_fp8_backward_workspace_bytes bytes for the same wishes, 16-byte

@@ -643,7 +643,9 @@ def dequantize_blocks(x, out=None, stream=None):
 def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     """out = a @ w.T (+ residual) in 8 bits: w [N, K] Fp8Blocks, a [M, K] Fp8Blocks
     or bf16 (any row stride; quantised per 128 values of a row on the way, into the
-    workspace); bf16 out, fp32 accumulation.  residual, out: [M, N] (any row
+    workspace); bf16 out, summed in fp32 of products that are cut, towards zero, below
+    2^-13 of the largest power of two among eight neighbouring ones (as
+    rc_linear_fp8_blocks says).  residual, out: [M, N] (any row
     stride; out may be residual as it lies).  What is given to write to (out, workspace) may lie
     beside the inputs in one buffer, but shares no memory with them.  A row's result does not depend on M for
     Fp8Blocks; a small bf16 call (up to 32 rows, or little work) sums in another order.
@@ -750,7 +752,8 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
                         stream=None):
     """The gradient of linear_fp8 for dy [M, N] bf16: x [M, K] Fp8Blocks, the input
     that the product has read; w [N, K] Fp8Blocks with their transposed form.
-    dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row;
+    dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row, its
+    products cut as linear_fp8's;
     dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual as it lies; otherwise dx,
     dw and workspace share no memory with the inputs or each other.  A workspace serves one
     call at a time.  Returns (dx, dw), None for what is not wanted (x and w may then be None)."""

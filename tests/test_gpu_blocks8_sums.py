@@ -1,0 +1,68 @@
+"""What the 8-bit products round before they sum, by products that cancel or whose
+sums are known to the last bit."""
+import pytest
+import torch
+
+import paper_2608_21229_amd as rc
+from tests import blocks8_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def one_product(at, k=128):
+    """Both forms of a product of one row and of w's first row, which hold the values of `at`
+    ({k: (a, w)}); a 448 that meets zeros makes every scale 1."""
+    a, w = torch.zeros(1, k), torch.zeros(8, k)
+    for i, (x, y) in at.items():
+        a[0, i], w[0, i] = x, y
+    for b in range(0, k, 128):
+        a[0, b + 100], w[1, b + 100] = 448.0, 448.0
+    a, w8 = a.bfloat16().cuda(), rc.quantize_blocks(w.bfloat16().cuda(), square=True, transposed=True)
+    a8 = rc.quantize_blocks(a)
+    assert (a8.exps[:, 0] == 127).all() and (w8.exps[:, 0] == 127).all()
+    # dx reads w_t as the product reads w: the columns of w are rows of dx's
+    t8 = rc.quantize_blocks(w.t().contiguous().bfloat16().cuda(), square=True, transposed=True)
+    dx = rc.linear_fp8_backward(a, None, t8, want_dw=False)[0]
+    return [float(t[0, 0]) for t in (rc.linear_fp8(a8, w8), rc.linear_fp8(a, w8), dx)]
+
+
+def split(power):
+    """2^power as a product of two codes, normal and subnormal ones."""
+    return [(2.0 ** s, 2.0 ** (power - s)) for s in range(-9, 9) if -9 <= power - s <= 8]
+
+
+@pytest.mark.parametrize("big", [(448.0, 448.0), (256.0, 1.0), (1.0, 1.0), (2.0 ** -6, 64.0), (2.0 ** -9, 256.0), (448.0, 2.0 ** -7)])
+@pytest.mark.parametrize("beside,cancel,k", [((0, 1), 70, 128), ((47, 40), 40 + 64, 128), ((250, 255), 8, 256)])
+def test_small_products_are_cut(big, beside, cancel, k):
+    """A large product, taken out by its negative in another group of eight, and a small one
+    beside it: what stays is the small one's multiples of 2^-13 of the large one's power of two."""
+    power = sum(int(torch.tensor(abs(c)).clamp(min=2.0 ** -6).log2().floor()) for c in big)
+    q = 2.0 ** (power - 13)
+    at = {beside[0]: big, cancel: (big[0], -big[1])}
+    seen = 0
+    for j in (power - 15, power - 13, power - 12, power - 8):
+        for a, w in split(j)[::5]:
+            for fa, fw in ((1.0, 1.0), (1.75, -1.0), (1.5, 1.25), (-1.125, 1.875)):
+                if min(a * abs(fa), w * abs(fw)) < 2.0 ** -6 and (fa, fw) != (1.0, 1.0):
+                    continue  # not a code
+                small = fa * a * fw * w
+                if max(a * abs(fa), w * abs(fw)) > 448:
+                    continue
+                want = float(torch.tensor(small / q).trunc()) * q
+                assert one_product({**at, beside[1]: (fa * a, fw * w)}, k) == [want] * 3, (j, a, w, fa, fw)
+                assert abs(want - small) < q
+                seen += want != small
+    assert seen > 0
+
+
+@pytest.mark.parametrize("other", [8, 15, 16, 32, 64, 120])
+def test_other_groups_of_eight_are_whole(other):
+    """What the large products meet is only their own eight, and zeros beside a large code count nothing."""
+    at = {0: (448.0, 448.0), 7: (448.0, -448.0)}
+    assert one_product({**at, other: (1.0, 1.0)}) == [1.0] * 3
+    assert one_product({**at, 3: (1.0, 1.0)}) == [0.0] * 3
+    assert one_product({5: (448.0, 0.0), 6: (0.0, 448.0), 3: (2.0 ** -9, 2.0 ** -5)}) == [2.0 ** -14] * 3
