@@ -480,7 +480,7 @@ size_t rc_gated_norm_backward_workspace_bytes(const rc_norm* d);  /* 0 on invali
  *   ld_exps  bytes, >= rows rounded up to 16, a multiple of 16; what it holds past the rows is unspecified
  * Quantisation: e is the smallest integer >= -127 with (largest finite magnitude of the block) * 2^-e <=
  * 448, 0 where that is 0; the code is the e4m3fn value nearest to x * 2^-e (ties to even; the product is
- * exact); infinities and NaN become NaN.
+ * exact); infinities and NaN become NaN.  Magnitudes from 1.9375 2^127 on become 2^128, more than bf16 holds.
  * Sizes: 0 <= rows <= 2^28, columns multiples of 8 from 8 to 2^22.  Pointers 16-byte aligned; row strides of
  * bf16 and fp32 matrices in elements, multiples of 8, <= 2^22.  Outputs overlap no input except as said.
  * A workspace serves one call at a time: calls and graph replays that may overlap need one each.
@@ -497,7 +497,7 @@ typedef struct {
 rc_status rc_quantize_blocks(int64_t M, int32_t K, const void* x, int64_t ldx, int32_t square,
                              const rc_blocks8* out, const rc_blocks8* out_t, void* stream);
 
-/* The values in bf16 (exact from 2^-133 on). */
+/* The values in bf16 (exact from 2^-133 on, infinite at 2^128). */
 rc_status rc_dequantize_blocks(int64_t M, int32_t K, const rc_blocks8* x, void* out, int64_t ldo, void* stream);
 
 /* out[m, n] = bf16( sum_k a[m, k] w[n, k] (+ r[m, n]) ) of the values of a [M, K] and w [N, K], summed in fp32
@@ -522,8 +522,8 @@ size_t rc_linear_fp8_workspace_bytes(int64_t M, int32_t N, int32_t K);  /* 0 on 
  *   dx [M, K] bf16  = sum_n dy[m, n] w[n, k] (+ r[m, k]): rc_linear_fp8 of dy, quantised in blocks of a row,
  *                     and w_t, the transposed weights [K, N] (products cut as there); NULL: not wanted, w_t and r
  *                     are then NULL
- *   dw [N, K] fp32  = sum_m dy[m, n] x[m, k], of dy as it is and of the values of x [M, K], the product's input,
- *                     which is its own checkpoint; zeros for M = 0; NULL: not wanted, x is then NULL
+ *   dw [N, K] fp32  = sum_m dy[m, n] x[m, k], of dy as it is and of the values of x [M, K] in bf16, the product's
+ *                     input, which is its own checkpoint; zeros for M = 0; NULL: not wanted, x is then NULL
  * r may be dx (same stride).  Workspace: rc_linear_fp8_backward_workspace_bytes bytes for the same wishes, 16-byte
  * aligned.  Deterministic: the sums over rows keep one order. */
 rc_status rc_linear_fp8_backward(int64_t M, int32_t N, int32_t K, const void* dy, int64_t lddy,

@@ -630,7 +630,7 @@ def quantize_blocks(x, square=False, transposed=False, out=None, stream=None) ->
 
 
 def dequantize_blocks(x, out=None, stream=None):
-    """The values of Fp8Blocks in bf16 [M, K] (exact).  Returns out."""
+    """The values of Fp8Blocks in bf16 [M, K] (exact below 2^128, infinite there).  Returns out."""
     M, K = _blocks(x, "x")
     dev, given = x.device, out is not None
     out, ldo = _rows_out(out, "out", M, K, dev, stream)
@@ -754,7 +754,7 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     that the product has read; w [N, K] Fp8Blocks with their transposed form.
     dx [M, K] bf16 = dy @ w (+ residual), dy quantised per 128 values of a row, its
     products cut as linear_fp8's;
-    dw [N, K] fp32 = dy.T @ x with dy as it is.  dx may be residual as it lies; otherwise dx,
+    dw [N, K] fp32 = dy.T @ x with dy as it is and x as dequantize_blocks expands it.  dx may be residual as it lies; otherwise dx,
     dw and workspace share no memory with the inputs or each other.  A workspace serves one
     call at a time.  Returns (dx, dw), None for what is not wanted (x and w may then be None)."""
     L, lddy, lddx, ldr, w_t = lib(), _rows_view(dy, "dy"), 0, 0, None

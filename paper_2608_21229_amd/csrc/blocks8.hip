@@ -128,7 +128,8 @@ __global__ __launch_bounds__(256) void quantize_squares_kernel(const Quant8Param
   }
 }
 
-// 8 codes per thread back to bf16, exact (4 significant bits) above bf16's smallest.
+// 8 codes per thread back to bf16, exact (4 significant bits) above bf16's smallest; the
+// largest code of the largest scale, 2^128, is infinite.
 // Memory-bound: 25 152 x 2560 takes 30 us (6.4 TB/s).
 __global__ __launch_bounds__(256) void dequantize_kernel(const Dequant8Params q) {
   const int g = q.K / 8;

@@ -2,7 +2,7 @@
 //
 //   dw[n, k] = sum_m dy[m, n] x[m, k],  x = code 2^e, dy in bf16, fp32 sums and result
 //
-// The codes are widened to bf16 (exact), so the product is one of
+// The codes are widened to bf16 (exact below 2^128), so the product is one of
 // v_mfma_f32_32x32x16_bf16.  The sum runs over rows, which both operands hold as
 // their slow dimension; they are transposed in registers on their way into LDS.
 #include <hip/hip_runtime.h>

@@ -66,3 +66,23 @@ def test_other_groups_of_eight_are_whole(other):
     assert one_product({**at, other: (1.0, 1.0)}) == [1.0] * 3
     assert one_product({**at, 3: (1.0, 1.0)}) == [0.0] * 3
     assert one_product({5: (448.0, 0.0), 6: (0.0, 448.0), 3: (2.0 ** -9, 2.0 ** -5)}) == [2.0 ** -14] * 3
+
+
+def test_largest_values():
+    """What is rounded up to 2^128, beyond bf16: finite in a product, infinite where it is widened to bf16."""
+    x = torch.zeros(9, 128)
+    x[0, 0], x[1, 0], x[2, 0], x[3, 1] = 1.9375 * 2.0 ** 127, -255 / 128 * 2.0 ** 127, 1.9296875 * 2.0 ** 127, 1.0
+    x, w = x.bfloat16().cuda(), torch.zeros(8, 128)
+    w[0, 0] = 2.0 ** -100
+    x8, w8 = rc.quantize_blocks(x), rc.quantize_blocks(w.bfloat16().cuda(), square=True)
+    assert x8.exps[0, :3].tolist() == [247] * 3 and plain.codes_of(x8)[:3, 0].tolist() == [256.0, -256.0, 240.0]
+    for a in (x, x8):
+        assert rc.linear_fp8(a, w8)[:3, 0].tolist() == [2.0 ** 28, -2.0 ** 28, 240 * 2.0 ** 20]
+    assert rc.dequantize_blocks(x8)[:3, 0].tolist() == [float("inf"), -float("inf"), 240 * 2.0 ** 120]
+    dy = torch.zeros(9, 8, device="cuda")
+    dy[2, 0], dy[3, 1], dy[0, 2], dy[1, 2] = 2.0 ** -100, 3.0, 1.0, -1.0
+    dw = rc.linear_fp8_backward(dy.bfloat16(), x8, None, want_dx=False)[1]
+    assert dw[:, 0].isnan()[[0, 1]].all() and not dw[:, 1:].isnan().any() and dw[1, 1] == 3.0
+    x8 = rc.quantize_blocks(x[2:])  # the largest that bf16 holds
+    dw = rc.linear_fp8_backward(dy[2:].bfloat16(), x8, None, want_dx=False)[1]
+    assert dw[0, 0] == 240 * 2.0 ** 20 and dw[1, 1] == 3.0 and dw[1, 0] == 0.0
