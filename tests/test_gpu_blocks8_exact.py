@@ -77,3 +77,52 @@ def test_inputs_gradient(m, n, k):
     for res in (None, r):
         dx, dw = rc.linear_fp8_backward(dy.bfloat16(), None, w8, residual=None if res is None else res.bfloat16(), want_dw=False)
         assert dw is None and torch.equal(dx, rounded(want if res is None else want + res))
+
+
+def test_gradient_against_differences():
+    """dx and dw are the derivatives of the product of the values: its change along a direction, which
+    is linear in each, so that halves of differences are exact.  dx of up to 128 is exact in bf16."""
+    m, n, k = 200, 128, 264
+    g = gen(7)
+    x, w, dy = whole(g, m, k), whole(g, n, k, 1), whole(g, m, n, 1)
+    w8 = rc.quantize_blocks(w.bfloat16(), square=True, transposed=True)
+    dx, dw = (t.double() for t in rc.linear_fp8_backward(dy.bfloat16(), rc.quantize_blocks(x.bfloat16()), w8))
+    f = lambda a, b: ((a @ b.t()) * dy).sum()  # noqa: E731
+    for _ in range(3):
+        # near the gradients, so that both changes are far from zero
+        u, v = whole(g, m, k) + 2 * (dy @ w).sign(), whole(g, n, k) + 2 * (dy.t() @ x).sign()
+        by = float(f(x + u, w) - f(x - u, w)) / 2
+        assert by == float((u * dx).sum()) and abs(by) > 100
+        by = float(f(x, w + v) - f(x, w - v)) / 2
+        assert by == float((v * dw).sum()) and abs(by) > 100
+
+
+def test_gradient_against_differences_of_ordinary_values():
+    """The same along directions near the gradients themselves, of normal values.  dy is what its quantisation
+    makes of it, so dx is off by its rounding, 2^-8 relative, by its products' cuts, each below 2^-13 of
+    the largest of eight, which is at most the largest |dy| times the largest |w| among them (all
+    eights hold normal codes), and by the sums, 2^-23 of the magnitudes a step: one for each 64 of n and the
+    8 values in one.  dw is off by its sums alone, a step for each 16 rows and the 16 in one, 64 where shares
+    are joined, and its rounding.  All are added as if of one sign."""
+    m, n, k = 300, 264, 136
+    g = gen(8)
+    randn = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    w8 = rc.quantize_blocks(randn(n, k).bfloat16(), square=True, transposed=True)
+    x8, dy8 = rc.quantize_blocks(randn(m, k).bfloat16()), rc.quantize_blocks(randn(m, n).bfloat16())
+    xv, wv, dy = (rc.dequantize_blocks(b) for b in (x8, w8, dy8))
+    dx, dw = (t.double() for t in rc.linear_fp8_backward(dy, x8, w8))
+    xv, wv, dy = xv.double(), wv.double(), dy.double()
+    f = lambda a, b: ((a @ b.t()) * dy).sum()  # noqa: E731
+    eight = lambda t: torch.nn.functional.pad(t.abs(), (0, -n % 8)).unflatten(1, (-1, 8)).amax(2)  # noqa: E731
+    cut = 2.0 ** -13 * 8 * (eight(dy) @ eight(wv.t()).t())   # certain, of each element of dx
+    for _ in range(3):
+        u, v = dy @ wv + 4 * randn(m, k).double(), dy.t() @ xv + 4 * randn(n, k).double()
+        by = float(f(xv + u, wv) - f(xv - u, wv)) / 2
+        sums = (n / 64 + 8) * 2.0 ** -23 * (dy.abs() @ wv.abs())
+        tol = float((u.abs() * (2.0 ** -8 * (dy @ wv).abs() + (cut + sums) * (1 + 2.0 ** -8))).sum())
+        assert tol < 0.1 * abs(by)
+        assert abs(by - float((u * dx).sum())) <= tol, (by, tol)
+        by = float(f(xv, wv + v) - f(xv, wv - v)) / 2
+        tol = (m / 16 + 80) * 2.0 ** -23 * float((v.abs() * (dy.abs().t() @ xv.abs())).sum())
+        assert tol < 0.1 * abs(by)
+        assert abs(by - float((v * dw).sum())) <= tol, (by, tol)
