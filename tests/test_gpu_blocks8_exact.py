@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2608_21229_amd as rc
+from tests.blocks8_plans import WEIGHT_GRADIENTS, workspace_bytes
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +127,22 @@ def test_gradient_against_differences_of_ordinary_values():
         tol = (m / 16 + 80) * 2.0 ** -23 * float((v.abs() * (dy.abs().t() @ xv.abs())).sum())
         assert tol < 0.1 * abs(by)
         assert abs(by - float((v * dw).sum())) <= tol, (by, tol)
+
+
+@pytest.mark.parametrize("plan", WEIGHT_GRADIENTS, ids=str)
+def test_weight_gradient(plan):
+    """Every kind of plan, over rows none of which is zero; what lies past the rows and columns of
+    a strided dy, and what a workspace held, stay out of it."""
+    m, n, k = plan[:3]
+    need = rc.lib().rc_linear_fp8_backward_workspace_bytes(m, n, k, 0, 1)
+    assert need == workspace_bytes(plan)
+    g = gen(m + n + k)
+    x = whole(g, m, k) * powers(g, m, k, torch.zeros(1, -(-k // 128), dtype=torch.int64, device=DEV), up=2)
+    dy = whole(g, m, n)
+    want = (dy.t() @ x).float()
+    assert float(want.abs().max()) < 2 ** 24
+    x8, buf = rc.quantize_blocks(x.bfloat16()), torch.full((m + 64, n + 64), float("nan"), dtype=torch.bfloat16, device=DEV)
+    dyb = buf[:m, :n].copy_(dy)
+    for ws in (None, torch.full((max(need, 1),), 255, dtype=torch.uint8, device=DEV)):
+        dw = torch.full((n, k), float("nan"), device=DEV)
+        assert torch.equal(rc.linear_fp8_backward(dyb, x8, None, dw=dw, want_dx=False, workspace=ws)[1], want)
