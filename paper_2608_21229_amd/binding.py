@@ -669,7 +669,7 @@ def linear_fp8(a, w, residual=None, out=None, workspace=None, stream=None):
     need = L.rc_linear_fp8_workspace_bytes(M, N, K)
     workspace, own = (_workspace(workspace, need, dev, stream) if need else None), workspace
     if need and workspace is own:
-        _apart_from(((own.data_ptr(), need, need, 1),), "workspace", a=a, w=w, residual=residual, out=out)
+        _apart_from((_place(own.data_ptr(), need, need, 1),), "workspace", a=a, w=w, residual=residual, out=out)
     _call(L.rc_linear_fp8, dev, stream, M, N, K, a.data_ptr(), lda, ctypes.byref(w.c), _ptr(residual), ldr,
           out.data_ptr(), ldo, _ptr(workspace), need)
     return out
@@ -685,51 +685,65 @@ def _rows_out(t, what, rows, cols, dev, stream):
 def _apart(out, what, ldo, a, name, residual, ldr):
     """Refuses the caller's output where it shares memory with the input a (None: no bf16 one), or with the
     residual other than as it lies."""
-    at = out.data_ptr()
-    if out.numel() == 0:
+    at, r = out.data_ptr(), None if residual is None else residual.data_ptr()
+    if a is None and (r is None or (r == at and ldr == ldo)):
         return
-    if a is not None and _meet(_rows_at(out), _rows_at(a)):
+    n, w = out.shape
+    if not n or not w:
+        return
+    end = at + 2 * ((n - 1) * ldo + w)
+    if a is not None and a.data_ptr() < end and _meet(_rows_at(out), _rows_at(a)):
         raise ValueError(f"{what} may not be {name}, which is read while it is written, nor overlap it")
-    if residual is None or (ldr == ldo and residual.data_ptr() == at):
+    if r is None:
         return
-    if residual.data_ptr() == at:
+    if r == at and ldr != ldo:
         raise ValueError(f"{what} may be residual only with its row stride, {ldr}, got {ldo}")
-    if _meet(_rows_at(out), _rows_at(residual)):
+    if r != at and r < end and at < r + 2 * ((n - 1) * ldr + w) and _meet(_rows_at(out), _rows_at(residual)):
         raise ValueError(f"{what} may be residual as it lies, but not overlap it otherwise")
 
 
 def _apart_from(t, what, **others):
     """Refuses a caller's output (a tensor or Fp8Blocks) or a workspace's place that shares memory with
     others, None where absent, which the call reads or writes too."""
-    mine = t if isinstance(t, tuple) else _places(t)
+    mine = t if type(t) is tuple else _places(t)
     for name, o in others.items():
-        if o is not None and any(_meet(a, b) for b in _places(o) for a in mine):
-            raise ValueError(f"{what} may not overlap {name}")
+        if o is None:
+            continue
+        for b in _places(o):
+            for a in mine:
+                if b[0] < a[4] and a[0] < b[4] and _meet(a, b):
+                    raise ValueError(f"{what} may not overlap {name}")
+
+
+def _place(p, width, stride, rows):
+    return p, width, stride, rows, p + (rows - 1) * stride + width
 
 
 def _rows_at(t):
-    """Where a tensor lies: (address, bytes of a row, bytes from one row to the next, rows).  One that
-    is no matrix is contiguous here: one row."""
-    size = t.element_size()
-    if t.dim() == 2 and not t.is_contiguous():
-        return t.data_ptr(), t.shape[1] * size, t.stride(0) * size, t.shape[0]
-    n = t.numel() * size
-    return t.data_ptr(), n, n, 1
+    """Where a tensor lies: its first byte, the bytes of a row, those from one row to the next, the rows, and
+    where it ends.  One that is no matrix is contiguous here: one row."""
+    p = t.data_ptr()
+    if t.is_contiguous():
+        n = t.nbytes
+        return p, n, n, 1, p + n
+    size = t.itemsize
+    return _place(p, t.shape[1] * size, t.stride(0) * size, t.shape[0])
 
 
 def _places(t):
     """The same of all that a tensor or Fp8Blocks (without their transposed form) hold."""
     if not isinstance(t, Fp8Blocks):
         return (_rows_at(t),)
-    codes, exps = t.shape[0] * t.c.ld, -(-t.shape[1] // 128) * t.c.ld_exps
-    return (t.c.codes or 0, codes, codes, 1), (t.c.exps or 0, exps, exps, 1)
+    c, (rows, cols) = t.c, t.shape
+    n, m, p, q = rows * c.ld, -(-cols // 128) * c.ld_exps, c.codes or 0, c.exps or 0
+    return (p, n, n, 1, p + n), (q, m, m, 1, q + m)
 
 
 def _meet(a, b):
     """Whether two places of _rows_at share a byte: their ranges do, and they are not columns side by
     side, which stay apart in every row where they do in one (modulo what divides both strides)."""
-    (p, w, s, n), (q, v, u, m) = a, b
-    if not (n and m and w and v) or p + (n - 1) * s + w <= q or q + (m - 1) * u + v <= p:
+    (p, w, s, n, end), (q, v, u, m, ends) = a, b
+    if not (n and m and w and v) or end <= q or ends <= p:
         return False
     g = math.gcd(s if n > 1 else 0, u if m > 1 else 0)
     r = (q - p) % g if g else 0
@@ -791,7 +805,7 @@ def linear_fp8_backward(dy, x, w, residual=None, dx=None, dw=None, want_dx=True,
     need = L.rc_linear_fp8_backward_workspace_bytes(M, N, K, int(want_dx), int(want_dw))
     workspace, own = (_workspace(workspace, need, dev, stream) if need else None), workspace
     if need and workspace is own:
-        _apart_from(((own.data_ptr(), need, need, 1),), "workspace", dy=dy, x=x if want_dw else None, w=w_t,
+        _apart_from((_place(own.data_ptr(), need, need, 1),), "workspace", dy=dy, x=x if want_dw else None, w=w_t,
                     residual=residual, dx=dx, dw=dw)
     _call(L.rc_linear_fp8_backward, dev, stream, M, N, K, dy.data_ptr(), lddy, ctypes.byref(x.c) if want_dw else None,
           ctypes.byref(w_t.c) if want_dx else None, _ptr(residual), ldr, _ptr(dx), lddx, _ptr(dw), K, _ptr(workspace), need)

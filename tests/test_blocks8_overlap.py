@@ -57,7 +57,7 @@ def test_places_by_their_bytes():
         places = []
         for stride in (rng.choice((24, 30)),) + (rng.choice((24, 30, 48)),):
             w, n = rng.randint(1, 24), rng.randint(1, 4)
-            places.append((rng.randint(0, 120), w, w if n == 1 else stride, n))
+            places.append(binding._place(rng.randint(0, 120), w, w if n == 1 else stride, n))
         a, b = places
         bytes_of = lambda t: {t[0] + i * t[2] + j for i in range(t[3]) for j in range(t[1])}  # noqa: E731
         meet = bool(bytes_of(a) & bytes_of(b))
@@ -85,7 +85,7 @@ def test_codes_and_exponents_in_one_pool():
         binding._apart_from(blocks_of(pool, end - 16, 40, 136), "out", x=x)
     # a workspace is what the call needs of it
     for need, fine in ((end, True), (end + 1, False)):
-        place = ((pool.data_ptr(), need, need, 1),)
+        place = (binding._place(pool.data_ptr(), need, need, 1),)
         if fine:
             binding._apart_from(place, "workspace", out=after)
         else:
