@@ -504,7 +504,7 @@ LinearPlan plan_linear(const LinearParams& q) {
 // part and a part per slice of 128 codes, in ns.  Measured at 20 slices (K = 2560): full
 // rounds of 256 x 256 39.8 us (one) and 434 (twelve), half rounds of 256 x 128,
 // 128 x 128 and 64 x 128 24.7, 15.4 and 10.6.  The choice, with its sides: 25 152 x 7680 x
-// 2560 434 us in 256 x 256, 464 in 192 x 256, 518 in 256 x 128; 4315 x 2560 x 2560 30.0 us
+// 2560 434 us in 256 x 256, 464 in 192 x 256, 518 in 256 x 128; 4315 x 2560 x 2560 (no residual) 30.0 us
 // in 230 tiles of 192 x 256, 32.5 in 170 of 256 x 256, 40.1 in two rounds of 256 x 128;
 // 600 x 2560 x 2560 10.4 us in 64 x 128, 13.5 in 128 x 128, 16.2 in two rounds of
 // 64 x 64, 28.7 in 256 x 256.
@@ -534,7 +534,7 @@ int32_t plan_linear8(int64_t M, int32_t N, int32_t K) {
 // 10 944 x 1280 x 1280 214 us in 25 tiles of 256 x 256, 51 in ten shares of each, 47 in
 // 50 tiles of 256 x 128 with five, 63 in 100 of 128 x 128 with two; 4840 x 2568 x 1928
 // 102 / 70 in one and two shares of 256 x 256, 67 in 176 whole tiles of 256 x 128;
-// 17 536 x 7680 x 2560 767 in 256 and 44 tiles, 561 with the 44 in five shares.
+// 17 536 x 7680 x 2560 767 in 256 and 44 tiles, 561 with the 44 in five shares and the join.
 WGrad8Plan plan_wgrad8(int64_t M, int32_t N, int32_t K) {
   struct {
     int64_t fixed, slice;

@@ -100,11 +100,14 @@ __device__ __forceinline__ void load_scales(uint32_t lds, const Blocks8& b, int6
 // ST slices of both operands, whose loads go out between the products of a step's
 // first half.
 //
-// 25 152 x 7680 x 2560 takes 434 us (2.28 PFLOP/s; the library's unscaled product
-// 474), 17 536 x 2560 x 7680 275 (2.51).  What it spends there: the matrix pipes are busy
-// 55% of the cycles, at a clock of 1.75 GHz.  With one operand row read for all, so that
-// every load hits, it takes 337 us, with one row written for all 380, with both 303
-// (equal rows also switch fewer bits, so the loads and stores cost at most that).
+// 25 152 x 7680 x 2560 takes 434-453 us (2.28-2.18 PFLOP/s, by boxes and inputs; the
+// library's unscaled product 474), 17 536 x 2560 x 7680 275-286 (2.51-2.41), in loops of
+// that call alone.  What it spends there: under counters, in a run of 493 us, the matrix pipes
+// are busy 55% of the cycles, at 1.74 GHz.  With one operand row read for all, so that
+// every load hits, it takes 337 us where it took 437, with one row written for all 380, with
+// both 303 (equal rows also switch fewer bits, so the loads and stores cost at most that).
+// A residual's loads go one after another at the tile's end: 4315 x 2560 x 2560
+// 31 us without and 34 with one, 25 152 x 2560 x 2560 147 and 185 (25 of them its bytes).
 // A form with one wave per SIMD, 128 x 128 accumulators per wave, the next operands
 // read between the products and stores left running over the next tile took the same
 // 435 (8192 cubed 386-404 against 404-411, but 4315 x 2560 x 2560 36 against 32); loads

@@ -64,9 +64,9 @@ __device__ __forceinline__ u32x4 column(const uint32_t (&r)[8]) {
 // What bounds it (256 x 256): 64 products of 32 cycles per slice and SIMD, 2048, and the
 // issue of what goes between them.  On 25 tiles, at 2.42 GHz, a slice takes 2 980 cycles
 // (counters: LDS busy 1 030 of them, waits 380, the rest waits for issue); on a full
-// chip, whose clock falls, 1.6 us: 17 536 x 4096 x 4096 runs in 439-456 us (1.29-1.34
+// chip, whose clock falls, 1.6 us: 17 536 x 4096 x 4096 runs in 439-460 us (1.28-1.34
 // PFLOP/s; the library's 8192 cubed reaches 1.43).  17 536 x 7680 x 2560, 300 tiles, takes
-// 558-564 us (the library's product of transposed dy 912).  Forms measured before, at these
+// 558-579 us with its join (the library's product of transposed dy 912).  Forms measured before, at these
 // two: dy loaded straight into LDS and both operands read by the transpose read
 // ds_read_b64_tr_b16, 443 and 591 us; both transposed in registers with one slice there,
 // 477 and 596; with two, 463 and 573 until the pieces behind a product became as short
